@@ -1,0 +1,476 @@
+"""Performance cases of the 4-bit paged prompt cache: page plans, stores and attention.
+
+A serving program that keeps prompts in 4 bits makes three kinds of calls.  A
+*plan* turns the requests' lengths into block tables and slot maps.  A *store*
+quantises the new rows of the keys and values into their slots, and reads them
+back as the values that they now stand for.  An *attention* pass lets each
+sequence's response rows attend to its cached keys, through its block table,
+and to the fresh 16- or 32-bit keys of the response.
+
+The cache holds e2m1 values (sign, two exponent bits, one mantissa bit; 0, .5,
+1, 1.5, 2, 3, 4, 6) with one power-of-two scale per 32 dimensions of a key or
+value.  One page of one head is, in bytes (T tokens, D dimensions):
+  keys         [T][D / 2]                two dimensions a byte, the even one low
+  values       [T / 8][16][8][D / 32]    8-token blocks; unit u holds dimensions u D/16 ..
+  key scales   [T][D / 32]               biased exponents (127 is one)
+  value scales [T / 8][D / 32][8]
+
+Widths, prompt lengths and response lengths are those of the workloads
+(``synth/workloads.py``) and of the prompt sweep, single tokens and contexts
+up to 128 Ki keys beside them.
+"""
+
+import math
+
+import torch
+
+own = False
+
+BLOCK = 32           # dimensions per scale
+E_MIN, E_MAX = -23, 13
+
+
+# -- cases ---------------------------------------------------------------------------------------
+def _plan(name, batch, lo, hi, grow, release, page, seed=0):
+    c = dict(kind="plan", batch=batch, len_lo=lo, len_hi=hi, grow=grow, release=release, page=page, length_seed=seed)
+    return dict(c, name=name) if name else c
+
+
+def _store(name, dtype, batch, lo, hi, heads, hd, page, seed=0, transposed=True):
+    c = dict(kind="store", dtype=dtype, batch=batch, len_lo=lo, len_hi=hi, heads=heads, hd=hd, page=page,
+             length_seed=seed, transposed=transposed)
+    return dict(c, name=name) if name else c
+
+
+def _attend(name, dtype, batch, lo, hi, rows, fresh, hq, hkv, hd, page, seed=0, ragged=False):
+    c = dict(kind="attend", dtype=dtype, batch=batch, len_lo=lo, len_hi=hi, rows=rows, fresh=fresh, hq=hq, hkv=hkv,
+             hd=hd, page=page, length_seed=seed, ragged=ragged)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one more token for each request of a full batch (launch latency)
+        _plan("plan_token_b64", 64, 1, 4096, 1, 0.0, 64),
+        # a large server's turn: prompts arrive, responses grow, finished and rolled-back requests return pages
+        _plan("plan_turn_b1024", 1024, 0, 8192, 2048, 0.25, 64, seed=1),
+        # the next token of 16 sequences enters the cache
+        _store("store_token_b16", "bf16", 16, 1, 1, 32, 128, 64, transposed=False),
+        # the prompts of the ragged serving batch, as a refresh leaves one layer's keys and (transposed) values
+        _store("store_prompt_ragged16", "bf16", 16, 681, 1971, 32, 128, 64, seed=176),
+        # few heads of 64 dimensions, odd lengths, fp32 model
+        _store("store_fp32_h4_d64", "fp32", 3, 57, 513, 4, 64, 32),
+        # the next token of 16 sequences, four key heads of seven query heads each
+        _attend("token_gqa_b16", "bf16", 16, 681, 1971, 1, False, 28, 4, 128, 64, seed=176),
+        # one token of one user over a short odd prompt, every head with keys of its own: the smallest call
+        _attend("token_p333", "bf16", 1, 333, 333, 1, False, 32, 32, 128, 32),
+        # long contexts: four users of up to 128 Ki tokens
+        _attend("token_long_b4", "bf16", 4, 70001, 131072, 1, False, 28, 4, 128, 256, seed=5),
+        # a short block of a response, ragged, with its own fresh keys
+        _attend("block8_gqa_b8", "bf16", 8, 129, 4096, 8, True, 28, 4, 128, 64, seed=3, ragged=True),
+        # one user with a long prompt: a cached denoising step
+        _attend("step_p4096", "bf16", 1, 4096, 4096, 256, True, 32, 32, 128, 64),
+        # a cached denoising step of the ragged serving batch
+        _attend("step_ragged16", "bf16", 16, 681, 1971, 256, True, 32, 32, 128, 64, seed=176),
+        # the tiny fp32 model's heads, a small ragged batch
+        _attend("step_fp32_d64", "fp32", 4, 64, 700, 32, True, 4, 4, 64, 32, seed=2, ragged=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    page = rng.choice([32, 64, 128, 256])
+    seed = rng.randint(0, 1 << 20)
+    u = rng.random()
+    if u < 0.2:
+        lo = rng.randint(0, 500)
+        return _plan(None, _log_int(rng, 1, 1024), lo, _log_int(rng, lo + 1, 8192), _log_int(rng, 1, 2048),
+                     rng.choice([0.0, 0.1, 0.4]), page, seed)
+    if u < 0.45:
+        dtype, hd = rng.choice(["bf16", "bf16", "fp32"]), rng.choice([64, 128])
+        batch, heads = _log_int(rng, 1, 16), rng.choice([1, 4, 7, 8, 32])
+        lo = _log_int(rng, 1, 1000)
+        return _store(None, dtype, batch, lo, _log_int(rng, lo, 1900), heads, hd, page, seed, rng.random() < 0.5)
+    hq, hkv = rng.choice([(32, 32), (28, 4), (16, 2), (7, 1), (8, 8), (4, 4), (12, 4)])
+    hd = rng.choice([64, 128, 128])
+    if u < 0.6:      # single tokens
+        batch = _log_int(rng, 1, 32)
+        lo = _log_int(rng, 1, 3000)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, max(lo, min(60000, 131072 * 4 // batch // hkv))), 1,
+                       rng.random() < 0.3, hq, hkv, hd, page, seed)
+    if u < 0.75:     # short blocks
+        batch = _log_int(rng, 1, 16)
+        lo = _log_int(rng, 1, 2000)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, 6000), rng.randint(2, 40), rng.random() < 0.7, hq, hkv,
+                       hd, page, seed, rng.random() < 0.5)
+    if u < 0.9:      # denoising steps
+        batch = _log_int(rng, 1, 12)
+        lo = _log_int(rng, 16, 1024)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, 2048), 8 * rng.randint(8, 32), True, hq, hkv, hd, page,
+                       seed, rng.random() < 0.3)
+    batch = rng.randint(1, 4)
+    lo = _log_int(rng, 1, 200)
+    return _attend(None, "fp32", batch, lo, _log_int(rng, lo, 1000), rng.choice([1, 5, 32, 64]), rng.random() < 0.7, 4,
+                   rng.choice([1, 2, 4]), hd, page, seed, rng.random() < 0.5)
+
+
+def _lengths(case):
+    """The sequences' cached lengths, a function of the case alone."""
+    g = torch.Generator().manual_seed(1000 + case["length_seed"])
+    lens = torch.randint(case["len_lo"], case["len_hi"] + 1, (case["batch"],), generator=g).tolist()
+    if case["batch"] > 1:
+        lens[0], lens[-1] = case["len_hi"], case["len_lo"]
+    return lens
+
+
+def _resp_lengths(case):
+    if not case["ragged"]:
+        return None
+    g = torch.Generator().manual_seed(2000 + case["length_seed"])
+    r = torch.randint(1, case["rows"] + 1, (case["batch"],), generator=g).tolist()
+    r[0] = case["rows"]
+    return r
+
+
+def _plan_lengths(case):
+    g = torch.Generator().manual_seed(1000 + case["length_seed"])
+    B = case["batch"]
+    old = torch.randint(case["len_lo"], case["len_hi"] + 1, (B,), generator=g)
+    new = old + (torch.randint(0, case["grow"] + 1, (B,), generator=g) if case["grow"] > 1 else 1)
+    u = torch.rand(B, generator=g)
+    half = torch.div(old, 2, rounding_mode="floor")
+    new = torch.where(u < case["release"] / 2, torch.zeros_like(old), torch.where(u < case["release"], half, new))
+    return old, new
+
+
+def _pages(n, page):
+    return (n + page - 1) // page
+
+
+def work(case):
+    if case["kind"] == "plan":
+        old, new = _plan_lengths(case)
+        moved = (_pages(old, case["page"]) - _pages(new, case["page"])).abs().sum().item()
+        grown = (new - old).clamp(min=0).sum().item()
+        # lengths in, moved pages from the queue to the table or back, row offsets and slots out
+        return {"bytes": 8 * case["batch"] + 8 * moved + 4 * (case["batch"] + 1) + 4 * grown + 20, "flops": 0}
+    if case["kind"] == "store":
+        n, e = sum(_lengths(case)), 2 if case["dtype"] == "bf16" else 4
+        values = 2 * n * case["heads"] * case["hd"]
+        # rows in, codes and scales out; codes and scales in, values out; the slot map twice
+        return {"bytes": 2 * values * e + 2 * (values // 2 + values // BLOCK) + 8 * n, "flops": 0}
+    lens, resp = _lengths(case), _resp_lengths(case)
+    resp = resp or [case["rows"]] * case["batch"]
+    e, out = (2, 2) if case["dtype"] == "bf16" else (4, 4)
+    hq, hkv, hd = case["hq"], case["hkv"], case["hd"]
+    fresh = resp if case["fresh"] else [0] * case["batch"]
+    by = sum(r * hq * hd * (e + out) + 2 * hkv * hd * e * f + 2 * hkv * (hd // 2 + hd // BLOCK) * n +
+             4 * _pages(n, case["page"]) + 4 for n, r, f in zip(lens, resp, fresh))
+    return {"bytes": by, "flops": sum(4 * r * (n + f) * hq * hd for n, r, f in zip(lens, resp, fresh))}
+
+
+# -- inputs --------------------------------------------------------------------------------------
+def _dtype(case):
+    return torch.float16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _page_bytes(page, hd):
+    return page * (hd + hd // 16)
+
+
+def _keys(shape, g, dev="cuda"):
+    """Rows of keys or values: normal, a few dimensions much larger than the others, as rotated keys have them."""
+    x = torch.randn(shape, generator=g, device=dev)
+    wide = torch.rand(shape[-1], generator=g, device=dev) < 0.05
+    return x * torch.where(wide, 4.0, 1.0)
+
+
+def _table(lens, page, spare, g):
+    """Block table over pages in random order, and the pages left over."""
+    need = [_pages(n, page) for n in lens]
+    n_pages = sum(need) + spare
+    order = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+    width = max(max(need), 1)
+    table = torch.full((len(lens), width), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, order[at:], n_pages
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s = dict(case=case)
+    page = case["page"]
+    if case["kind"] == "plan":
+        old, new = _plan_lengths(case)
+        have, want = _pages(old, page), _pages(new, page)
+        n_pages = int((have + (want - have).clamp(min=0)).sum()) + 7
+        width = int(torch.maximum(have, want).max()) + 3
+        order = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+        table = torch.full((case["batch"], width), -1, dtype=torch.int32, device="cuda")
+        j = torch.arange(width, device="cuda")
+        used = j[None] < have.cuda()[:, None]
+        table[used] = order[:int(have.sum())]
+        rest = n_pages - int(have.sum())
+        head = int(torch.randint(0, n_pages, (1,), generator=g, device="cuda"))
+        free = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+        free[(head + torch.arange(rest, device="cuda")) % n_pages] = order[n_pages - rest:]
+        rows = int((new - old).clamp(min=0).sum())
+        s.update(old=old.to(torch.int32).cuda(), new=new.to(torch.int32).cuda(), table=table, free=free, n_pages=n_pages,
+                 pool=torch.tensor([head, rest], dtype=torch.int32, device="cuda"), rows=(rows + 63) // 64 * 64 + 64)
+        return s
+    hd = case["hd"]
+    lens = _lengths(case)
+    heads = case["heads"] if case["kind"] == "store" else case["hkv"]
+    table, _, n_pages = _table(lens, page, 3, g)
+    # one page more than the cache has: the plain form's place for rows without a slot
+    data = torch.zeros(n_pages + 1, heads, _page_bytes(page, hd), dtype=torch.uint8, device="cuda")
+    s.update(data=data, n_pages=n_pages, lut=_values("cuda"), lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    if case["kind"] == "store":
+        n = sum(lens)
+        pos = torch.cat([torch.arange(x, device="cuda") for x in lens])
+        seq = torch.repeat_interleave(torch.arange(len(lens), device="cuda"), s["lens"].long())
+        slots = table[seq, pos // page].long() * page + pos % page
+        s["slots"] = torch.cat([slots, slots.new_full((5,), -1)]).to(torch.int32)   # a padded row map
+        rows = (n + 5 + 63) // 64 * 64
+        k = _keys((heads, rows, hd), g).to(_dtype(case))
+        v = _keys((heads, rows, hd), g).to(_dtype(case))
+        s["k"] = k[:, :n + 5]
+        # the values as the prompt cache holds them: transposed, seen row by row
+        s["v"] = v.transpose(1, 2).contiguous().transpose(1, 2)[:, :n + 5] if case["transposed"] else v[:, :n + 5]
+        return s
+    for a in range(0, n_pages, 256):
+        n = min(256, n_pages - a)
+        k, v = _keys((n, heads, page, hd), g), _keys((n, heads, page, hd), g)
+        data[a:a + n] = _pack(*_quantise(k), *_quantise(v))
+    G, B = case["rows"], case["batch"]
+    pad = (G + 7) // 8 * 8
+    s.update(table=table, q=(torch.randn(case["hq"], B * G, hd, generator=g, device="cuda") * 2).to(_dtype(case)),
+             max_cached=max(lens), stride=pad, k2=None, vt2=None, resp=None,
+             out=torch.zeros(B * G, case["hq"] * hd, device="cuda",
+                             dtype=torch.bfloat16 if case["dtype"] == "bf16" else torch.float32))
+    if case["fresh"]:
+        ld = (B * pad + 63) // 64 * 64
+        s["k2"] = _keys((heads, ld, hd), g).to(_dtype(case))
+        s["vt2"] = _keys((heads, hd, ld), g).to(_dtype(case))
+    resp = _resp_lengths(case)
+    if resp:
+        s["resp"] = torch.tensor(resp, dtype=torch.int32, device="cuda")
+    return s
+
+
+# -- the plain forms -----------------------------------------------------------------------------
+def _values(dev):
+    half = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=dev)
+    return torch.cat([half, -half])
+
+
+def _quantise(x):
+    """e2m1 codes (one a byte) and biased scale exponents of x [..., D], per 32 dimensions.
+
+    The scale is the smallest power of two whose range reaches the block's
+    largest magnitude to within half a step: at most 7 steps of the largest
+    code 6.  Every operation here is exact in 32 bits."""
+    x = x.float()
+    b = x.unflatten(-1, (-1, BLOCK))
+    top = b.abs().amax(-1)
+    m, e = torch.frexp(top)
+    e = torch.where(m > 0.875, e - 2, e - 3)
+    e = torch.where(top == 0, torch.full_like(e, E_MIN), e).clamp(E_MIN, E_MAX)
+    y = b.abs() * _two_to(-e)[..., None]
+    step = torch.where(y < 2, 0.5, torch.where(y < 4, 1.0, 2.0))
+    y = (torch.round(y / step) * step).clamp(max=6.0)          # ties to even
+    code = torch.where(y < 2, y * 2, torch.where(y < 4, y + 2, y * 0.5 + 4)).to(torch.uint8)
+    return (code + 8 * torch.signbit(b).to(torch.uint8)).flatten(-2), (e + 127).to(torch.uint8)
+
+
+def _two_to(e):
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
+
+
+def _pack(kc, ks, vc, vs):
+    """Codes and scales [n][heads][T][...] to page bytes [n][heads][page bytes]."""
+    n, h, T, D = kc.shape
+    kb = kc[..., 0::2] | kc[..., 1::2] << 4
+    vb = (vc[..., 0::2] | vc[..., 1::2] << 4).view(n, h, T // 8, 8, 16, D // 32).transpose(3, 4)
+    vs = vs.view(n, h, T // 8, 8, D // BLOCK).transpose(3, 4)
+    return torch.cat([t.reshape(n, h, -1) for t in (kb, vb, ks, vs)], -1)
+
+
+def _unpack(data, page, D, lut):
+    """Page bytes [...][page bytes] to the keys and values [...][T][D] that they stand for, in 32 bits."""
+    half, sc = page * D // 2, page * D // BLOCK
+    k, v, ks, vs = data.split([half, half, sc, sc], -1)
+    ks = ks.unflatten(-1, (page, D // BLOCK))
+    vs = vs.unflatten(-1, (page // 8, D // BLOCK, 8)).transpose(-1, -2).flatten(-3, -2)
+    k = lut[torch.stack([k & 15, k >> 4], -1).int()].flatten(-2).unflatten(-1, (page, D))
+    v = torch.stack([v & 15, v >> 4], -1).flatten(-2).unflatten(-1, (page // 8, 16, 8, D // 16))
+    v = lut[v.transpose(-2, -3).reshape(*data.shape[:-1], page, D).int()]
+    spread = lambda t: _two_to(t.int() - 127).repeat_interleave(BLOCK, -1)  # noqa: E731
+    return k * spread(ks), v * spread(vs)
+
+
+def _plan_plain(s):
+    page, old, new, n = s["case"]["page"], s["old"].long(), s["new"].long(), s["n_pages"]
+    have, want = _pages(old, page), _pages(new, page)
+    pops, pushes, grow = (want - have).clamp(min=0), (have - want).clamp(min=0), (new - old).clamp(min=0)
+    before = lambda x: x.cumsum(0) - x  # noqa: E731
+    head, count = s["pool"][0].long(), s["pool"][1].long()
+    width = s["table"].shape[1]
+    j = torch.arange(width, device="cuda")[None]
+    have, want = have[:, None], want[:, None]
+    page_in = s["free"][(head + before(pops)[:, None] + j - have) % n]
+    table = torch.where((j >= have) & (j < want), page_in, s["table"])
+    at = (head + count + before(pushes)[:, None] + j - want) % n
+    at = torch.where((j >= want) & (j < have), at, n).flatten()
+    free = torch.cat([s["free"], s["free"][:1]]).scatter(0, at, s["table"].flatten())[:n]
+    npop, npush = pops.sum(), pushes.sum()
+    pool = torch.stack([(head + npop) % n, count - npop + npush]).to(torch.int32)
+    off = torch.cat([grow.new_zeros(1), grow.cumsum(0)])
+    t = torch.arange(s["rows"], device="cuda")
+    b = torch.searchsorted(off[1:], t, right=True).clamp(max=len(old) - 1)
+    p = old[b] + t - off[b]
+    slot = table[b, (p // page).clamp(max=width - 1)] * page + p % page
+    slots = torch.where(t < off[-1], slot, -1).to(torch.int32)
+    short = (npop > count).to(torch.int32).reshape(1)
+    return {"table": table, "free": free, "pool": pool, "row_off": off.to(torch.int32), "slots": slots, "status": short}
+
+
+def _store_plain(s):
+    page, data, hd = s["case"]["page"], s["data"], s["case"]["hd"]
+    slot = s["slots"].long()
+    where_ = torch.where(slot >= 0, slot, s["n_pages"] * page)
+    p, o = where_ // page, where_ % page
+    half, sc = page * hd // 2, page * hd // BLOCK
+    k, v, ks, vs = data.split([half, half, sc, sc], -1)
+    kc, ke = _quantise(s["k"])
+    vc, ve = _quantise(s["v"])
+    rows = lambda t: t.transpose(0, 1)  # noqa: E731
+    k.unflatten(-1, (page, hd // 2))[p, :, o] = rows(kc[..., 0::2] | kc[..., 1::2] << 4)
+    ks.unflatten(-1, (page, hd // BLOCK))[p, :, o] = rows(ke)
+    v.unflatten(-1, (page // 8, 16, 8, hd // 32))[p, :, o // 8, :, o % 8] = \
+        rows((vc[..., 0::2] | vc[..., 1::2] << 4).unflatten(-1, (16, -1)))
+    vs.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8] = rows(ve)
+    # back again: the values that the stored rows stand for
+    take = dict(k=k.unflatten(-1, (page, hd // 2))[p, :, o], ks=ks.unflatten(-1, (page, hd // BLOCK))[p, :, o],
+                v=v.unflatten(-1, (page // 8, 16, 8, hd // 32))[p, :, o // 8, :, o % 8].flatten(-2),
+                vs=vs.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8])
+    out = {}
+    for n in ("k", "v"):
+        x = s["lut"][torch.stack([take[n] & 15, take[n] >> 4], -1).flatten(-2).int()]
+        x = x * _two_to(take[n + "s"].int() - 127).repeat_interleave(BLOCK, -1)
+        out[n] = torch.where((slot >= 0)[:, None, None], x, 0.0).transpose(0, 1).to(_dtype(s["case"])).contiguous()
+    return out
+
+
+def _attend_plain(s):
+    c = s["case"]
+    page, hd, hkv, B, G = c["page"], c["hd"], c["hkv"], c["batch"], c["rows"]
+    k, v = _unpack(s["data"][s["table"].clamp(min=0).long()], page, hd, s["lut"])     # [B][pages][heads][T][D]
+    k, v = (t.transpose(1, 2).flatten(2, 3)[:, :, :s["max_cached"]] for t in (k, v))
+    ok = torch.arange(k.shape[2], device="cuda")[None] < s["lens"][:, None]
+    n_resp = s["resp"] if s["resp"] is not None else torch.full_like(s["lens"], G)
+    if c["fresh"]:
+        cut = lambda t: t[:, :B * s["stride"]].float().view(hkv, B, s["stride"], hd)[:, :, :G].transpose(0, 1)  # noqa: E731
+        k, v = torch.cat([k, cut(s["k2"])], 2), torch.cat([v, cut(s["vt2"].transpose(1, 2).contiguous())], 2)
+        ok = torch.cat([ok, torch.arange(G, device="cuda")[None] < n_resp[:, None]], 1)
+    q = s["q"].float().view(hkv, -1, B, G, hd).permute(2, 0, 1, 3, 4).reshape(B, hkv, -1, hd)
+    z = torch.matmul(q, k.transpose(2, 3).contiguous()) / math.sqrt(hd)
+    z = z.masked_fill(~ok[:, None, None], -math.inf)
+    m = z.amax(-1, keepdim=True).clamp(min=-3e38)       # a row without keys gives zeros
+    p = torch.exp(z - m)
+    o = torch.matmul(p, v) / p.sum(-1, keepdim=True).clamp(min=1e-38)
+    o = o.view(B, hkv, -1, G, hd).permute(0, 3, 1, 2, 4).reshape(B, G, -1)
+    o = torch.where((torch.arange(G, device="cuda")[None] < n_resp[:, None])[..., None], o, 0.0)
+    return o.reshape(B * G, -1).to(s["out"].dtype)
+
+
+def run(s):
+    c = s["case"]
+    if not own:
+        return {"plan": _plan_plain, "store": _store_plain, "attend": _attend_plain}[c["kind"]](s)
+    from paper_2608_08086_amd import archer
+    if c["kind"] == "plan":
+        pool, off, slots, status = archer.cache4_plan(s["old"], s["new"], c["page"], s["table"], s["free"], s["pool"],
+                                                      s["rows"])
+        return {"table": s["table"], "free": s["free"], "pool": pool, "row_off": off, "slots": slots, "status": status}
+    cache = archer.Cache4(s["data"][:s["n_pages"]], c["page"], c["hd"])
+    if c["kind"] == "store":
+        archer.cache4_write(cache, s["k"], s["v"], s["slots"])
+        k, v = archer.cache4_read(cache, s["slots"], _dtype(c))
+        return {"k": k, "v": v}
+    return archer.op_attention_cache4(s["q"], cache, s["table"], s["lens"], s["max_cached"], K2=s["k2"], Vt2=s["vt2"],
+                                      fresh_stride=s["stride"], resp_len=s["resp"], O=s["out"])
+
+
+# -- the definition in 64 bits -------------------------------------------------------------------
+def _stored(x):
+    """What x [..., D] is after it was stored, from the definition: per 32 dimensions the power of two, the nearest
+    e2m1 magnitude, ties to the even code."""
+    x = x.double()
+    b = x.view(*x.shape[:-1], -1, 32)
+    top = b.abs().max(-1, keepdim=True).values
+    scale = torch.full_like(top, 2.0 ** E_MIN)
+    for e in range(E_MIN, E_MAX):
+        scale = torch.where(top > 7 * 2.0 ** e, 2.0 ** (e + 1), scale)
+    y = b.abs() / scale
+    code = (y > 0.25).int() + (y >= 0.75).int() + (y > 1.25).int() + (y >= 1.75).int() + (y > 2.5).int() + \
+        (y >= 3.5).int() + (y > 5.0).int()
+    mag = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=x.device)[code.long()]
+    return (torch.copysign(mag, b) * scale).reshape(x.shape)
+
+
+def _token(data, page, D, pages, at):
+    """Keys and values of one sequence, token by token from their bytes: [heads][n][D] in 64 bits."""
+    d = data[pages]                                              # [n][heads][bytes]
+    n, H, _ = d.shape
+    dim = torch.arange(D, device=d.device)
+    val = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device=d.device)
+    a = at[:, None]
+    k_at = a * (D // 2) + dim // 2
+    unit = dim // (D // 16)
+    inside = dim % (D // 16)
+    v_at = page * D // 2 + ((a // 8 * 16 + unit) * 8 + a % 8) * (D // 32) + inside // 2
+    ks_at = page * D + a * (D // 32) + dim // 32
+    vs_at = page * D + page * D // 32 + (a // 8 * (D // 32) + dim // 32) * 8 + a % 8
+    pick = lambda i: torch.gather(d, 2, i[:, None].expand(n, H, D))  # noqa: E731
+    low = (dim % 2 == 0)
+    out = []
+    for c_at, s_at in ((k_at, ks_at), (v_at, vs_at)):
+        c = pick(c_at)
+        c = torch.where(low, c % 16, c // 16)
+        out.append((val[c.long()] * torch.pow(2.0, pick(s_at).double() - 127)).transpose(0, 1))
+    return out
+
+
+def exact(case, seed):
+    if case["kind"] == "plan":
+        return None
+    s = prepare(case, seed)
+    page, hd = case["page"], case["hd"]
+    if case["kind"] == "store":
+        live = (s["slots"] >= 0)[None, :, None]
+        return {n: torch.where(live, _stored(s[n]), 0.0) for n in ("k", "v")}
+    B, G, hkv, grp = case["batch"], case["rows"], case["hkv"], case["hq"] // case["hkv"]
+    resp = _resp_lengths(case) or [G] * B
+    out = torch.zeros(B * G, case["hq"] * hd, dtype=torch.float64, device="cuda")
+    for b, n in enumerate(_lengths(case)):
+        r = resp[b]
+        for h in range(hkv):
+            pos = torch.arange(n, device="cuda")
+            k, v = _token(s["data"][:, h:h + 1], page, hd, s["table"][b, pos // page].long(), pos % page)
+            k, v = k[0], v[0]
+            if case["fresh"]:
+                at = slice(b * s["stride"], b * s["stride"] + r)
+                k = torch.cat([k, s["k2"][h, at].double()])
+                v = torch.cat([v, s["vt2"][h, :, at].double().T])
+            q = s["q"][h * grp:(h + 1) * grp, b * G:b * G + r].double().reshape(-1, hd)
+            p = torch.softmax(q @ k.T.contiguous() / math.sqrt(hd), -1)
+            o = (p @ v).view(grp, r, hd).transpose(0, 1).reshape(r, -1)
+            out[b * G:b * G + r, h * grp * hd:(h + 1) * grp * hd] = o
+    return out
