@@ -12,7 +12,7 @@ The cache holds e2m1 values (sign, two exponent bits, one mantissa bit; 0, .5,
 value.  One page of one head is, in bytes (T tokens, D dimensions):
   keys         [T][D / 2]                two dimensions a byte, the even one low
   values       [T / 8][16][8][D / 32]    8-token blocks; unit u holds dimensions u D/16 ..
-  key scales   [T][D / 32]               biased exponents (127 is one)
+  key scales   [T / 8][D / 32][8]        biased exponents (127 is one)
   value scales [T / 8][D / 32][8]
 
 Widths, prompt lengths and response lengths are those of the workloads
@@ -298,7 +298,7 @@ def _pack(kc, ks, vc, vs):
     n, h, T, D = kc.shape
     kb = kc[..., 0::2] | kc[..., 1::2] << 4
     vb = (vc[..., 0::2] | vc[..., 1::2] << 4).view(n, h, T // 8, 8, 16, D // 32).transpose(3, 4)
-    vs = vs.view(n, h, T // 8, 8, D // BLOCK).transpose(3, 4)
+    ks, vs = (t.view(n, h, T // 8, 8, D // BLOCK).transpose(3, 4) for t in (ks, vs))
     return torch.cat([t.reshape(n, h, -1) for t in (kb, vb, ks, vs)], -1)
 
 
@@ -306,8 +306,7 @@ def _unpack(data, page, D, lut):
     """Page bytes [...][page bytes] to the keys and values [...][T][D] that they stand for, in 32 bits."""
     half, sc = page * D // 2, page * D // BLOCK
     k, v, ks, vs = data.split([half, half, sc, sc], -1)
-    ks = ks.unflatten(-1, (page, D // BLOCK))
-    vs = vs.unflatten(-1, (page // 8, D // BLOCK, 8)).transpose(-1, -2).flatten(-3, -2)
+    ks, vs = (t.unflatten(-1, (page // 8, D // BLOCK, 8)).transpose(-1, -2).flatten(-3, -2) for t in (ks, vs))
     k = lut[torch.stack([k & 15, k >> 4], -1).int()].flatten(-2).unflatten(-1, (page, D))
     v = torch.stack([v & 15, v >> 4], -1).flatten(-2).unflatten(-1, (page // 8, 16, 8, D // 16))
     v = lut[v.transpose(-2, -3).reshape(*data.shape[:-1], page, D).int()]
@@ -352,12 +351,13 @@ def _store_plain(s):
     vc, ve = _quantise(s["v"])
     rows = lambda t: t.transpose(0, 1)  # noqa: E731
     k.unflatten(-1, (page, hd // 2))[p, :, o] = rows(kc[..., 0::2] | kc[..., 1::2] << 4)
-    ks.unflatten(-1, (page, hd // BLOCK))[p, :, o] = rows(ke)
+    ks.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8] = rows(ke)
     v.unflatten(-1, (page // 8, 16, 8, hd // 32))[p, :, o // 8, :, o % 8] = \
         rows((vc[..., 0::2] | vc[..., 1::2] << 4).unflatten(-1, (16, -1)))
     vs.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8] = rows(ve)
     # back again: the values that the stored rows stand for
-    take = dict(k=k.unflatten(-1, (page, hd // 2))[p, :, o], ks=ks.unflatten(-1, (page, hd // BLOCK))[p, :, o],
+    take = dict(k=k.unflatten(-1, (page, hd // 2))[p, :, o],
+                ks=ks.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8],
                 v=v.unflatten(-1, (page // 8, 16, 8, hd // 32))[p, :, o // 8, :, o % 8].flatten(-2),
                 vs=vs.unflatten(-1, (page // 8, hd // BLOCK, 8))[p, :, o // 8, :, o % 8])
     out = {}
@@ -436,8 +436,8 @@ def _token(data, page, D, pages, at):
     unit = dim // (D // 16)
     inside = dim % (D // 16)
     v_at = page * D // 2 + ((a // 8 * 16 + unit) * 8 + a % 8) * (D // 32) + inside // 2
-    ks_at = page * D + a * (D // 32) + dim // 32
-    vs_at = page * D + page * D // 32 + (a // 8 * (D // 32) + dim // 32) * 8 + a % 8
+    ks_at = page * D + (a // 8 * (D // 32) + dim // 32) * 8 + a % 8
+    vs_at = ks_at + page * D // 32
     pick = lambda i: torch.gather(d, 2, i[:, None].expand(n, H, D))  # noqa: E731
     low = (dim % 2 == 0)
     out = []
