@@ -79,6 +79,104 @@ archer_status archer_op_attention_noalloc(int32_t dtype, int32_t Mq, int32_t Hq,
                                           int32_t ld1, const void *K2, const void *Vt2, int32_t nk2,
                                           int32_t ld2, void *O, void *hip_stream);
 
+/* ---- 4-bit paged prompt cache -------------------------------------------------
+ * One layer's keys and values in e2m1 (sign, two exponent bits, one mantissa
+ * bit: 0, .5, 1, 1.5, 2, 3, 4, 6) with one power-of-two scale per 32
+ * dimensions: 136 instead of 512 bytes per token and head of 128 dimensions.
+ * Tokens live in pages of page_size tokens; a slot is
+ * page * page_size + position in the page, and a sequence's row of a block
+ * table lists its pages in order.  Several sequences may list the same page.
+ *
+ * data: device, 16-byte aligned, archer_cache4_bytes bytes, caller-owned.
+ * [n_pages][n_kv_heads] blocks of page_size * (head_dim + head_dim / 16) bytes:
+ *   keys    [page_size][head_dim / 2]             byte j: dimensions 2j (low nibble), 2j + 1
+ *   values  [page_size / 8][16][8][head_dim / 32] unit u: dimensions u head_dim / 16 ..
+ *   key scales, then value scales [page_size / 8][head_dim / 32][8]   exponent + 127
+ * page_size 32, 64, 128 or 256; head_dim 64 or 128; n_pages * page_size < 2^31. */
+typedef struct {
+  void *data;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+} archer_cache4;
+
+/* Bytes of the cache's data (0 and last_error for a bad shape; data is not read). */
+size_t archer_cache4_bytes(const archer_cache4 *cache);
+
+/* Block tables, free pages and the slots of new rows for requests whose
+ * lengths change from len_old[b] to len_new[b] (device int32 [batch]; batch <=
+ * 4096): a request that grows takes pages, one that shrinks (rollback, or 0:
+ * finished) gives its last ones back.  One call, no synchronisation.
+ *   table       [batch][max_pages], in place: entries below ceil(len_old / page_size)
+ *               are the request's pages; the taken ones are appended, all others
+ *               (those given back too) stay as they are
+ *   free_pages  [n_pages], in place: a ring of the free pages
+ *   pool_in     [2]: index of the ring's first free page, number of free pages
+ *   pool_out    [2]: the same after the call; must not alias pool_in
+ *   row_off     [batch + 1]: prefix sums of the rows added, max(len_new - len_old, 0)
+ *   slot_map    [slot_rows]: the slot of every added row, request by request, then -1
+ *   status      [1]: 0, or why nothing was changed (pool_out = pool_in, row_off 0,
+ *               slot_map -1): 1 too few free pages, 2 a length is negative or beyond
+ *               max_pages, 3 more than slot_rows rows, 4 the pool is inconsistent
+ * Pages are taken from the ring's front in request order and given back behind
+ * its end, those of this call for later ones.  Called again with the same
+ * arguments it gives the same results.  The arrays must not overlap. */
+archer_status archer_cache4_plan(int32_t batch, const int32_t *len_old, const int32_t *len_new,
+                                 int32_t page_size, int32_t n_pages, int32_t max_pages, int32_t *table,
+                                 int32_t *free_pages, const int32_t *pool_in, int32_t *pool_out,
+                                 int32_t *row_off, int32_t *slot_map, int32_t slot_rows, int32_t *status,
+                                 void *hip_stream);
+
+/* Store rows of keys and values (fp16 for ARCHER_BF16, fp32 for ARCHER_FP32) in
+ * the slots slot_map[row]; rows whose slot is outside the cache (-1) are
+ * skipped.  Slots of one call must be distinct (of rows that share one, an
+ * unspecified mixture is stored); rows >= 0.  Element (head, row, d) is at
+ * K[head k_head + row k_row + d] and V[head v_head + row v_row + d v_dim] (strides in
+ * elements, any sign), with v_dim = 1 or v_row = 1: the prompt cache's
+ * transposed values are stored as they lie (else ARCHER_E_UNSUPPORTED).
+ * Per 32 dimensions the scale is 2^e, e the least integer with max |x| <= 7 * 2^e,
+ * clamped to [-23, 13]; elements are rounded to the nearest e2m1 value of
+ * x / 2^e, ties to the even code, and saturate at 6 * 2^e (49152 at most).  Every
+ * stored element is exact in fp16.  A NaN makes its 32 elements NaN. */
+archer_status archer_cache4_write(int32_t dtype, const archer_cache4 *cache, int32_t rows, const void *K,
+                                  int64_t k_head, int64_t k_row, const void *V, int64_t v_head,
+                                  int64_t v_row, int64_t v_dim, const int32_t *slot_map, void *hip_stream);
+
+/* The stored elements of the slots slot_map[row], as fp16 (ARCHER_BF16) or
+ * fp32 (ARCHER_FP32): K and V [n_kv_heads][rows][head_dim], 16-byte aligned.
+ * Rows whose slot is outside the cache become zeros.  Slots may repeat. */
+archer_status archer_cache4_read(int32_t dtype, const archer_cache4 *cache, int32_t rows,
+                                 const int32_t *slot_map, void *K, void *V, void *hip_stream);
+
+/* The anchored attention with the cached segment in 4 bits, for a batch: row i of
+ * sequence b attends to the sequence's cached keys, positions 0 ..
+ * cached_len[b] - 1 through row b of the block table, and, where K2 is given, to the
+ * sequence's fresh keys; no other mask, scale 1 / sqrt(hd).  Types and heads
+ * as archer_op_attention (hd and Hkv are the cache's).
+ *   Q          [Hq][batch G][hd]: G query rows per sequence
+ *   O          [batch G][Hq hd]: a row without any key gives zeros
+ *   table      device int32 [batch][max_pages]; the keys of an entry outside
+ *              [0, n_pages) are left out
+ *   cached_len device int32 [batch], >= 0; no more than max_cached (host; sizes the
+ *              launch) and max_pages * page_size keys are read
+ *   K2, Vt2    [Hkv][ld2][hd], [Hkv][hd][ld2], or both NULL: sequence b's fresh keys
+ *              are rows b fresh_stride .. + resp_len[b] - 1; ld2 and fresh_stride multiples of
+ *              8, fresh_stride >= G, batch fresh_stride <= ld2
+ *   resp_len   device int32 [batch] in [0, G], or NULL (G each): the sequence's
+ *              query rows and fresh keys; rows of O from resp_len[b] on stay as they are
+ * A single token per sequence is G = 1, its key stored beforehand (K2 NULL) or
+ * fresh.  Q, K2, Vt2 and O 16-byte aligned.  workspace: device scratch of
+ * archer_op_attention_cache4_ws_bytes bytes, 256-byte aligned (NULL if that is
+ * 0); calls sharing a workspace must not overlap.  A row's result does not depend on
+ * the other sequences' data, but on batch and max_cached, which choose the
+ * split of the keys, to rounding. */
+size_t archer_op_attention_cache4_ws_bytes(int32_t dtype, int32_t batch, int32_t G, int32_t Hq, int32_t Hkv,
+                                           int32_t hd, int32_t max_cached, int32_t fresh);
+archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4 *cache, int32_t batch, int32_t G,
+                                         int32_t Hq, const void *Q, const int32_t *table, int32_t max_pages,
+                                         const int32_t *cached_len, int32_t max_cached, const void *K2,
+                                         const void *Vt2, int32_t ld2, int32_t fresh_stride,
+                                         const int32_t *resp_len, void *O, void *workspace, size_t ws_bytes,
+                                         void *hip_stream);
+
 /* Kernel classes for timing.  The projection classes _QKV, _O, _GATEUP and
  * _DOWN are the launches of CachedForward passes (M = G per sequence); their
  * _FULL twins are the same projections in FullForward (refresh) passes

@@ -38,6 +38,8 @@ EXPORTED = [
     "archer_pack_weight", "archer_session_begin", "archer_session_advance", "archer_session_response",
     "archer_session_state_bytes", "archer_session_save", "archer_session_restore", "archer_read_state",
     "archer_set_single_term", "archer_op_attention_noalloc", "archer_op_projection_tiles",
+    "archer_cache4_bytes", "archer_cache4_plan", "archer_cache4_write", "archer_cache4_read",
+    "archer_op_attention_cache4_ws_bytes", "archer_op_attention_cache4",
 ]
 FORWARD_CONTROLLER, FORWARD_REFRESH, FORWARD_CACHED = 0, 1, 2
 READ_LOGITS, READ_HIDDEN, READ_RESIDUAL, READ_PROMPT_K, READ_PROMPT_V = range(5)
@@ -80,6 +82,11 @@ class DecodeCfg(C.Structure):
 class Trace(C.Structure):
     _fields_ = [("refreshed", C.c_void_p), ("dist", C.c_void_p), ("age", C.c_void_p),
                 ("unmask_pos", C.c_void_p), ("unmask_tok", C.c_void_p), ("remask_pos", C.c_void_p)]
+
+
+class Cache4Desc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32)]
 
 
 P = C.c_void_p
@@ -134,6 +141,20 @@ lib.archer_op_attention_noalloc.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c
 lib.archer_op_projection_tiles.restype = C.c_int
 lib.archer_op_projection_tiles.argtypes = [C.POINTER(ModelCfg), C.POINTER(Limits), C.c_int32, C.c_int32, C.c_int32,
                                            C.c_int32, C.c_char_p, C.c_size_t]
+lib.archer_cache4_bytes.restype = C.c_size_t
+lib.archer_cache4_bytes.argtypes = [C.POINTER(Cache4Desc)]
+lib.archer_cache4_plan.restype = C.c_int
+lib.archer_cache4_plan.argtypes = [C.c_int32, P, P, C.c_int32, C.c_int32, C.c_int32, P, P, P, P, P, P, C.c_int32, P, P]
+lib.archer_cache4_write.restype = C.c_int
+lib.archer_cache4_write.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, P, C.c_int64, C.c_int64, P, C.c_int64,
+                                    C.c_int64, C.c_int64, P, P]
+lib.archer_cache4_read.restype = C.c_int
+lib.archer_cache4_read.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, P, P, P, P]
+lib.archer_op_attention_cache4_ws_bytes.restype = C.c_size_t
+lib.archer_op_attention_cache4_ws_bytes.argtypes = [C.c_int32] * 8
+lib.archer_op_attention_cache4.restype = C.c_int
+lib.archer_op_attention_cache4.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, C.c_int32, C.c_int32, P, P,
+                                           C.c_int32, P, C.c_int32, P, P, C.c_int32, C.c_int32, P, P, P, C.c_size_t, P]
 lib.archer_timing_begin.restype = C.c_int
 lib.archer_timing_begin.argtypes = [P, C.c_uint32, C.c_int32]
 lib.archer_timing_end.restype = C.c_int
@@ -479,4 +500,138 @@ def op_attention_noalloc(Q, K1, Vt1, nk1, K2, Vt2, nk2, dtype=BF16, O=None):
         O = torch.empty(Mq, Hq * hd, dtype=torch_dtype(dtype), device="cuda")
     _check(lib.archer_op_attention_noalloc(dtype, Mq, Hq, Hkv, hd, _ptr(Q), _ptr(K1), _ptr(Vt1), nk1, ld1,
                                            _ptr(K2), _ptr(Vt2), nk2, ld2, _ptr(O), _stream()))
+    return O
+
+
+# -- the 4-bit paged prompt cache of archer_ops.h -------------------------------------------------
+def _refuse(status, msg):
+    raise ArcherError(status, msg)
+
+
+def _dev(t, dtype, name, strided=False):
+    """Device pointer of a tensor that the call reads or writes on the current device."""
+    if t.dtype != dtype:
+        _refuse(E_ARG, f"{name} must be {dtype}")
+    if t.get_device() != torch.cuda.current_device():
+        _refuse(E_ARG, f"{name} must be on the current CUDA device")
+    if not strided and not t.is_contiguous():
+        _refuse(E_ARG, f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _i32(t, n, name):
+    p = _dev(t, torch.int32, name)
+    if t.numel() != n:
+        _refuse(E_SHAPE, f"{name} must have {n} elements")
+    return p
+
+
+class Cache4:
+    """One layer's 4-bit paged cache (archer_cache4): data uint8 [n_pages][n_kv_heads][page bytes]."""
+
+    def __init__(self, data, page_size, head_dim):
+        if data.dim() != 3:
+            _refuse(E_SHAPE, "data must be [n_pages][n_kv_heads][page bytes]")
+        self.data = data
+        self.n_pages, self.n_kv_heads, page_bytes = data.shape
+        self.page_size, self.head_dim = page_size, head_dim
+        self.desc = Cache4Desc(_dev(data, torch.uint8, "data"), self.n_pages, page_size, self.n_kv_heads, head_dim)
+        n = lib.archer_cache4_bytes(C.byref(self.desc))
+        if n == 0:
+            _refuse(E_SHAPE, lib.archer_last_error().decode())
+        if n != data.numel():
+            _refuse(E_SHAPE, f"a page of {page_size} tokens has {page_size * (head_dim + head_dim // 16)} bytes "
+                             f"per head, not {page_bytes}")
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim):
+        return cls(torch.zeros(n_pages, n_kv_heads, page_size * (head_dim + head_dim // 16), dtype=torch.uint8,
+                               device="cuda"), page_size, head_dim)
+
+
+def cache4_plan(len_old, len_new, page_size, table, free_pages, pool, slot_rows):
+    """archer_cache4_plan: table [B][max_pages] and free_pages [n_pages] change in place; returns the new
+    pool [2], row_off [B + 1], slot_map [slot_rows] and status [1] (int32 tensors; nothing synchronises)."""
+    B = len_old.numel()
+    if table.dim() != 2 or table.shape[0] != B:
+        _refuse(E_SHAPE, "table must be [batch][max_pages]")
+    n_pages, width = free_pages.numel(), table.shape[1]
+    dev = dict(dtype=torch.int32, device=len_old.device)
+    pool_out, status = torch.empty(2, **dev), torch.empty(1, **dev)
+    row_off, slot_map = torch.empty(B + 1, **dev), torch.empty(max(slot_rows, 0), **dev)
+    _check(lib.archer_cache4_plan(B, _i32(len_old, B, "len_old"), _i32(len_new, B, "len_new"), page_size, n_pages, width,
+                                  _i32(table, B * width, "table"), _i32(free_pages, n_pages, "free_pages"),
+                                  _i32(pool, 2, "pool"), pool_out.data_ptr(), row_off.data_ptr(), slot_map.data_ptr(),
+                                  slot_rows, status.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    return pool_out, row_off, slot_map, status
+
+
+def _cache4_dtype(t, name):
+    if t == torch.float16:
+        return BF16
+    if t != torch.float32:
+        _refuse(E_ARG, f"{name} must be torch.float16 (bf16 models) or torch.float32")
+    return FP32
+
+
+def cache4_write(cache, K, V, slot_map):
+    """archer_cache4_write: K, V [n_kv_heads][rows][head_dim] (views; K with unit stride along the last
+    dimension, V along the last or the row dimension) into the slots slot_map [rows]."""
+    dt = _cache4_dtype(K.dtype, "K")
+    rows = slot_map.numel()
+    shape = (cache.n_kv_heads, rows, cache.head_dim)
+    if K.shape != shape or V.shape != shape:
+        _refuse(E_SHAPE, f"K and V must be {list(shape)}")
+    (kh, kr, kd), (vh, vr, vd) = K.stride(), V.stride()
+    if kd != 1:
+        _refuse(E_UNSUPPORTED, "K must have unit stride along its dimensions")
+    _check(lib.archer_cache4_write(dt, C.byref(cache.desc), rows, _dev(K, K.dtype, "K", True), kh, kr,
+                                   _dev(V, K.dtype, "V", True), vh, vr, vd, _i32(slot_map, rows, "slot_map"),
+                                   torch.cuda.current_stream().cuda_stream))
+
+
+def cache4_read(cache, slot_map, dtype=torch.float16):
+    """archer_cache4_read: the stored rows of slot_map, K and V [n_kv_heads][rows][head_dim]."""
+    dt = _cache4_dtype(dtype, "dtype")
+    rows = slot_map.numel()
+    K = torch.empty(cache.n_kv_heads, rows, cache.head_dim, dtype=dtype, device=cache.data.device)
+    V = torch.empty_like(K)
+    _check(lib.archer_cache4_read(dt, C.byref(cache.desc), rows, _i32(slot_map, rows, "slot_map"), K.data_ptr(),
+                                  V.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    return K, V
+
+
+def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=None, fresh_stride=0, resp_len=None, O=None):
+    """archer_op_attention_cache4: Q [Hq][B G][hd] (fp16: O bf16; fp32: O fp32), table [B][max_pages], cached_len [B],
+    optional fresh K2 [Hkv][ld2][hd] and Vt2 [Hkv][hd][ld2], optional resp_len [B].  Returns O [B G][Hq hd]
+    (preallocated if given: rows past resp_len are not written)."""
+    dt = _cache4_dtype(Q.dtype, "Q")
+    if Q.dim() != 3 or table.dim() != 2:
+        _refuse(E_SHAPE, "Q must be [Hq][B G][hd], table [B][max_pages]")
+    (Hq, rows, hd), (B, width) = Q.shape, table.shape
+    if B < 1 or rows % B or hd != cache.head_dim:
+        _refuse(E_SHAPE, "Q must hold G rows of head_dim for every row of the table")
+    G, Hkv = rows // B, cache.n_kv_heads
+    k2 = v2 = None
+    ld2 = 0
+    if K2 is not None or Vt2 is not None:
+        if K2 is None or Vt2 is None or K2.dim() != 3:
+            _refuse(E_ARG, "K2 and Vt2 must both be given, or neither")
+        ld2 = K2.shape[1]
+        if K2.shape != (Hkv, ld2, hd) or Vt2.shape != (Hkv, hd, ld2):
+            _refuse(E_SHAPE, "K2 must be [Hkv][ld2][hd] and Vt2 [Hkv][hd][ld2]")
+        k2, v2 = _dev(K2, Q.dtype, "K2"), _dev(Vt2, Q.dtype, "Vt2")
+    otype = torch_dtype(dt)
+    if O is None:
+        O = torch.empty(rows, Hq * hd, dtype=otype, device=Q.device)
+    elif O.shape != (rows, Hq * hd):
+        _refuse(E_SHAPE, "O must be [B G][Hq hd]")
+    nbytes = lib.archer_op_attention_cache4_ws_bytes(dt, B, G, Hq, Hkv, hd, max_cached, int(k2 is not None))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+    _check(lib.archer_op_attention_cache4(dt, C.byref(cache.desc), B, G, Hq, _dev(Q, Q.dtype, "Q"),
+                                          _i32(table, B * width, "table"), width, _i32(cached_len, B, "cached_len"),
+                                          max_cached, k2, v2, ld2, fresh_stride,
+                                          None if resp_len is None else _i32(resp_len, B, "resp_len"),
+                                          _dev(O, otype, "O"), ws.data_ptr() if nbytes else None, nbytes,
+                                          torch.cuda.current_stream().cuda_stream))
     return O

@@ -1,0 +1,387 @@
+// Page plans of the 4-bit prompt cache, and the kernels that store rows of
+// keys and values in it and read them back (layout: cache4.h).
+#include <algorithm>
+
+#include "cache4.h"
+
+// ---------------------------------------------------------------------------
+// Page plan.  Requests change their lengths from len_old to len_new; with
+// pages(n) = ceil(n / T), request b keeps the first min(pages(old),
+// pages(new)) entries of its table row, takes pages(new) - pages(old) pages
+// from the free ring when it grows, and gives its last ones back when it
+// shrinks.  Three exclusive prefix sums over the requests (pages taken, pages
+// given back, rows added) place everything:
+//   page r taken       = ring[(head + r) mod n]
+//   page k given back -> ring[(head + count + k) mod n]
+//   new row of position p: slot = page(p / T) * T + p mod T
+// The ring entries read lie in [head, head + count), those written behind
+// them, so no order between workgroups is needed and the call may be repeated
+// with the same result.  Every workgroup makes the sums for itself (a few
+// thousand numbers from L2: 2 us) rather than wait for one that does, and
+// takes the slots from the sums, not from the table that others are writing.
+constexpr int PLAN_THREADS = 256;
+constexpr int PLAN_ROWS = 4;     // slots a thread makes with one search
+
+__device__ __forceinline__ long long wave_scan_i64(long long v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long t = __shfl_up(v, o, 64);
+    if (lane >= o) v += t;
+  }
+  return v;
+}
+
+// largest b in [0, n) with off[b] <= v
+__device__ __forceinline__ int scan_find(const int* off, int n, int v) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (off[mid] <= v) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void cache4_plan_kernel(C4PlanArgs a) {
+  extern __shared__ int sh[];
+  const int B = a.batch, tid = threadIdx.x, T = 1 << a.psh;
+  int* taken = sh;               // exclusive sums, [B + 1] each
+  int* given = sh + (B + 1);
+  int* rows = sh + 2 * (B + 1);
+  __shared__ long long part[3][PLAN_THREADS / 64];
+  __shared__ int bad_len;
+  if (tid == 0) bad_len = 0;
+  __syncthreads();
+
+  const long long cap = (long long)a.width << a.psh;
+  const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+  // totals in 64 bits: lengths far beyond the table must not wrap into it
+  long long st = 0, sg = 0, sr = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int o = a.len_old[b], n = a.len_new[b];
+    if (o < 0 || n < 0 || o > cap || n > cap) bad_len = 1;
+    const int have = (int)(((long long)o + T - 1) >> a.psh), want = (int)(((long long)n + T - 1) >> a.psh);
+    st += max(want - have, 0);
+    sg += max(have - want, 0);
+    sr += max((long long)n - o, 0LL);
+  }
+  const int w = tid >> 6, lane = tid & 63;
+  const long long it = wave_scan_i64(st), ig = wave_scan_i64(sg), ir = wave_scan_i64(sr);
+  if (lane == 63) { part[0][w] = it; part[1][w] = ig; part[2][w] = ir; }
+  __syncthreads();
+  long long bt = it - st, bg = ig - sg, br = ir - sr, tt = 0, tg = 0, tr = 0;
+#pragma unroll
+  for (int i = 0; i < PLAN_THREADS / 64; ++i) {
+    if (i < w) { bt += part[0][i]; bg += part[1][i]; br += part[2][i]; }
+    tt += part[0][i]; tg += part[1][i]; tr += part[2][i];
+  }
+  const int head = a.pool_in[0], count = a.pool_in[1];
+  int status = 0;
+  if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages) status = 4;
+  else if (bad_len) status = 2;
+  else if (tg > a.n_pages - count) status = 4;      // more pages than there are
+  else if (tt > count) status = 1;
+  else if (tr > a.slot_rows) status = 3;
+  const int total = status ? 0 : (int)tr;
+  if (!status) {
+    for (int b = b0; b < b1; ++b) {
+      const int o = a.len_old[b], n = a.len_new[b];
+      const int have = (int)(((long long)o + T - 1) >> a.psh), want = (int)(((long long)n + T - 1) >> a.psh);
+      taken[b] = (int)bt; given[b] = (int)bg; rows[b] = (int)br;
+      bt += max(want - have, 0);
+      bg += max(have - want, 0);
+      br += max(n - o, 0);
+    }
+    if (tid == 0) { taken[B] = (int)tt; given[B] = (int)tg; rows[B] = (int)tr; }
+  }
+  __syncthreads();
+
+  const int gid = blockIdx.x * PLAN_THREADS + tid, gsz = gridDim.x * PLAN_THREADS;
+  if (gid == 0) {
+    *a.status = status;
+    a.pool_out[0] = status ? head : (int)(((long long)head + tt) % a.n_pages);
+    a.pool_out[1] = status ? count : (int)(count - tt + tg);
+  }
+  for (int b = gid; b <= B; b += gsz) a.row_off[b] = status ? 0 : rows[b];
+  if (!status) {
+    for (int r = gid; r < (int)tt; r += gsz) {
+      const int b = scan_find(taken, B, r);
+      const int have = (a.len_old[b] + T - 1) >> a.psh;
+      a.table[(size_t)b * a.width + have + r - taken[b]] = a.free_pages[((long long)head + r) % a.n_pages];
+    }
+    for (int r = gid; r < (int)tg; r += gsz) {
+      const int b = scan_find(given, B, r);
+      const int want = (a.len_new[b] + T - 1) >> a.psh;
+      a.free_pages[((long long)head + count + r) % a.n_pages] = a.table[(size_t)b * a.width + want + r - given[b]];
+    }
+  }
+  for (long long r0 = (long long)gid * PLAN_ROWS; r0 < a.slot_rows; r0 += (long long)gsz * PLAN_ROWS) {
+    int s[PLAN_ROWS];
+    int b = r0 < total ? scan_find(rows, B, (int)r0) : 0;
+#pragma unroll
+    for (int e = 0; e < PLAN_ROWS; ++e) {
+      const int r = (int)r0 + e;
+      s[e] = -1;
+      if (r0 + e < total) {
+        while (r >= rows[b + 1]) ++b;              // ends: rows[B] = total > r
+        const int o = a.len_old[b], p = o + r - rows[b], j = p >> a.psh, have = (o + T - 1) >> a.psh;
+        const int page = j < have ? a.table[(size_t)b * a.width + j]
+                                  : a.free_pages[((long long)head + taken[b] + j - have) % a.n_pages];
+        if (page >= 0 && page < a.n_pages) s[e] = (page << a.psh) + (p & (T - 1));
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < PLAN_ROWS; ++e)
+      if (r0 + e < a.slot_rows) a.slots[r0 + e] = s[e];
+  }
+}
+
+void launch_cache4_plan(const C4PlanArgs& a, hipStream_t st) {
+  const long items = std::max<long>((long)(a.slot_rows + PLAN_ROWS - 1) / PLAN_ROWS, a.batch);
+  const unsigned grid = (unsigned)std::min<long>(std::max<long>((items + PLAN_THREADS - 1) / PLAN_THREADS, 1), 512);
+  cache4_plan_kernel<<<grid, PLAN_THREADS, 3 * (a.batch + 1) * sizeof(int), st>>>(a);
+}
+
+// ---------------------------------------------------------------------------
+// Store.  Per 32 dimensions: top = max |x|, the scale 2^e with e the least
+// integer that has top <= 7 * 2^e (so the largest element moves by no more
+// than half a step of its own binade), e clamped to [-23, 13], and each element the nearest
+// e2m1 value of x / 2^e, ties to the even code, beyond 6 saturating.  All of
+// it is exact in fp32, and the rounding is the hardware's own conversion.
+//
+// A thread owns 8 dimensions of 8 consecutive rows: as a value unit that is
+// (D = 128) 32 consecutive bytes, and either orientation of the source gives it
+// 16-byte loads (row-major: 8 dimensions of one row; transposed: 8 rows of one dimension).
+// The four threads of a scale block share a row quad (row-major) or the four
+// 16-lane groups of a wave (transposed).
+__device__ __forceinline__ unsigned quad_max_u32(unsigned v) {
+  v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true));   // lanes xor 1
+  return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true));   // lanes xor 2
+}
+__device__ __forceinline__ unsigned group_max_u32(unsigned v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((unsigned)a[0], (unsigned)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((unsigned)b[0], (unsigned)b[1]);
+}
+
+// 8 consecutive elements in fp32, n of them readable; vec: 16-byte loads are allowed
+template <class T>
+__device__ __forceinline__ void load8(const T* p, long step, int n, bool vec, float* x) {
+  if (vec && n == 8) {
+    if constexpr (sizeof(T) == 2) {
+      const f16x8 v = __builtin_bit_cast(f16x8, *(const u32x4*)p);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+    } else {
+      const f32x4 v = *(const f32x4*)p, u = *(const f32x4*)(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { x[e] = v[e]; x[4 + e] = u[e]; }
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = e < n ? to_f32(p[e * step]) : 0.f;
+}
+
+template <class T, int HD, bool TRANS>
+__device__ __forceinline__ void cache4_store(const C4RowsArgs& a, const T* src, long s_row, long s_dim, bool vec,
+                                             bool value) {
+  constexpr int U = HD / 8;                        // threads across a row
+  const int tid = threadIdx.x, h = blockIdx.y;
+  const int unit = TRANS ? (tid >> 4) % U : tid % U;
+  const int oct = TRANS ? (tid & 15) + 16 * ((tid >> 4) / U) : tid / U;
+  const long r0 = ((long)blockIdx.x * (256 / U) + oct) * 8;
+  // threads past the last row stay for the reductions
+  const int n = (int)min(8L, max(0L, a.rows - r0));
+  int slot[8];
+  const long nslots = (long)a.c.n_pages << a.c.psh;
+  bool run = n == 8;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    slot[r] = r < n ? a.slots[r0 + r] : -1;
+    if (slot[r] < 0 || slot[r] >= nslots) slot[r] = -1;
+    run = run && slot[r] == slot[0] + r;
+  }
+  run = run && slot[0] >= 0 && (slot[0] & 7) == 0;   // an aligned 8-token block
+
+  float x[8][8];                                   // [row][dimension]
+  if constexpr (TRANS) {
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      float t[8];
+      load8(src + (unit * 8 + d) * s_dim + r0, 1, n, vec, t);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) x[r][d] = t[r];
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load8(src + (r0 + r) * s_row + unit * 8 * s_dim, s_dim, r < n ? 8 : 0, vec, x[r]);
+  }
+
+  unsigned code[8], eb[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    unsigned top = 0;                              // |x| as integers: NaN above infinity above the rest
+#pragma unroll
+    for (int d = 0; d < 8; ++d) top = max(top, __float_as_uint(x[r][d]) & 0x7fffffffu);
+    top = TRANS ? group_max_u32(top) : quad_max_u32(top);
+    // top = 1.m 2^E: e = E - 2, and one more when 1.m > 1.75
+    unsigned e = (top + 0x1fffffu) >> 23;
+    e = min(max(e, (unsigned)C4_EMIN + 2u), (unsigned)C4_EMAX + 2u) - 2u;
+    const float sc = __uint_as_float(e << 23);
+    unsigned c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][0], x[r][1], sc, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][2], x[r][3], sc, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][4], x[r][5], sc, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][6], x[r][7], sc, 3);
+    code[r] = c;
+    eb[r] = top > 0x7f800000u ? (unsigned)C4_NAN : e;
+  }
+
+  using L = C4<HD>;
+  const int T_ = 1 << a.c.psh;
+  const size_t pb = L::page_bytes(T_);
+  const bool first = (unit & 3) == 0;              // the thread that stores the block's scale
+  const int g = unit >> 2;
+  if (run) {
+    const int t0 = slot[0] & (T_ - 1);
+    uint8_t* page = a.c.data + ((size_t)(slot[0] >> a.c.psh) * a.c.hkv + h) * pb;
+    if (value) {
+      u32x4 lo, hi;
+      if constexpr (HD == 128) {
+        lo = u32x4{code[0], code[1], code[2], code[3]};
+        hi = u32x4{code[4], code[5], code[6], code[7]};
+      } else {                                     // units 2u and 2u + 1: the low and the high half of the codes
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo[i] = __builtin_amdgcn_perm(code[2 * i + 1], code[2 * i], 0x05040100u);
+          hi[i] = __builtin_amdgcn_perm(code[2 * i + 1], code[2 * i], 0x07060302u);
+        }
+      }
+      u32x4* d = (u32x4*)(page + L::voff(T_) + (t0 >> 3) * L::VBLK + unit * 32);
+      d[0] = lo;
+      d[1] = hi;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) *(unsigned*)(page + (size_t)(t0 + r) * L::KROW + unit * 4) = code[r];
+    }
+    if (first) {
+      u32x2 s = {eb[0] | eb[1] << 8 | eb[2] << 16 | eb[3] << 24, eb[4] | eb[5] << 8 | eb[6] << 16 | eb[7] << 24};
+      *(u32x2*)(page + (value ? L::vsoff(T_) : L::ksoff(T_)) + (t0 >> 3) * L::SBLK + g * 8) = s;
+    }
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    if (slot[r] < 0) continue;
+    const int t = slot[r] & (T_ - 1);
+    uint8_t* page = a.c.data + ((size_t)(slot[r] >> a.c.psh) * a.c.hkv + h) * pb;
+    if (!value) {
+      *(unsigned*)(page + (size_t)t * L::KROW + unit * 4) = code[r];
+    } else if constexpr (HD == 128) {
+      *(unsigned*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 4) = code[r];
+    } else {
+      uint16_t* d = (uint16_t*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 2);
+      d[0] = (uint16_t)code[r];
+      d[8] = (uint16_t)(code[r] >> 16);
+    }
+    if (first) page[(value ? L::vsoff(T_) : L::ksoff(T_)) + (t >> 3) * L::SBLK + g * 8 + (t & 7)] = (uint8_t)eb[r];
+  }
+}
+
+template <class T>
+__device__ __forceinline__ bool aligned16(const void* p, long a, long b) {
+  return (((uintptr_t)p | (uintptr_t)(a * (long)sizeof(T)) | (uintptr_t)(b * (long)sizeof(T))) & 15) == 0;
+}
+
+template <class T, int HD, bool VT>
+__global__ __launch_bounds__(256) void cache4_write_kernel(C4RowsArgs a) {
+  const int h = blockIdx.y;
+  if (blockIdx.z == 0) {
+    cache4_store<T, HD, false>(a, (const T*)a.K + h * a.k_head, a.k_row, 1, aligned16<T>(a.K, a.k_head, a.k_row), false);
+  } else if constexpr (VT) {
+    cache4_store<T, HD, true>(a, (const T*)a.V + h * a.v_head, 1, a.v_dim, aligned16<T>(a.V, a.v_head, a.v_dim), true);
+  } else {
+    cache4_store<T, HD, false>(a, (const T*)a.V + h * a.v_head, a.v_row, 1, aligned16<T>(a.V, a.v_head, a.v_row), true);
+  }
+}
+
+// Read back: the same thread-to-row map (row-major), each row's 8 dimensions
+// one or two 16-byte stores.
+template <class T, int HD>
+__global__ __launch_bounds__(256) void cache4_read_kernel(C4RowsArgs a) {
+  constexpr int U = HD / 8;
+  using L = C4<HD>;
+  const int tid = threadIdx.x, h = blockIdx.y, unit = tid % U, g = unit >> 2;
+  const bool value = blockIdx.z != 0;
+  const long r0 = ((long)blockIdx.x * (256 / U) + tid / U) * 8;
+  const int n = (int)min(8L, max(0L, a.rows - r0));
+  const int T_ = 1 << a.c.psh;
+  const size_t pb = L::page_bytes(T_);
+  const long nslots = (long)a.c.n_pages << a.c.psh;
+  T* out = (T*)(value ? a.Vo : a.Ko) + ((size_t)h * a.rows + r0) * HD + unit * 8;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    if (r >= n) break;
+    const int slot = a.slots[r0 + r];
+    unsigned c = 0, e = 0;
+    if (slot >= 0 && slot < nslots) {
+      const int t = slot & (T_ - 1);
+      const uint8_t* page = a.c.data + ((size_t)(slot >> a.c.psh) * a.c.hkv + h) * pb;
+      if (!value) {
+        c = *(const unsigned*)(page + (size_t)t * L::KROW + unit * 4);
+      } else if constexpr (HD == 128) {
+        c = *(const unsigned*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 4);
+      } else {
+        const uint16_t* p = (const uint16_t*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 2);
+        c = p[0] | (unsigned)p[8] << 16;
+      }
+      e = page[(value ? L::vsoff(T_) : L::ksoff(T_)) + (t >> 3) * L::SBLK + g * 8 + (t & 7)];
+    }
+    const float sc = __uint_as_float(e << 23);     // 255: every element NaN
+    if constexpr (sizeof(T) == 2) {
+      u32x4 v;
+      v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 0));
+      v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 1));
+      v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 2));
+      v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 3));
+      *(u32x4*)(out + (size_t)r * HD) = v;
+    } else {
+      const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1);
+      const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3);
+      *(f32x4*)(out + (size_t)r * HD) = f32x4{p0[0], p0[1], p1[0], p1[1]};
+      *(f32x4*)(out + (size_t)r * HD + 4) = f32x4{p2[0], p2[1], p3[0], p3[1]};
+    }
+  }
+}
+
+template <class T, int HD>
+static void write_t(const C4RowsArgs& a, dim3 grid, hipStream_t st) {
+  if (a.v_dim == 1) cache4_write_kernel<T, HD, false><<<grid, 256, 0, st>>>(a);
+  else cache4_write_kernel<T, HD, true><<<grid, 256, 0, st>>>(a);
+}
+
+static dim3 rows_grid(int hd, const C4RowsArgs& a) {
+  const int per = 256 / (hd / 8) * 8;
+  return dim3((unsigned)((a.rows + (long)per - 1) / per), (unsigned)a.c.hkv, 2);
+}
+
+int launch_cache4_write(int fp32, int hd, const C4RowsArgs& a, hipStream_t st) {
+  const dim3 grid = rows_grid(hd, a);
+  if (fp32) hd == 128 ? write_t<float, 128>(a, grid, st) : write_t<float, 64>(a, grid, st);
+  else hd == 128 ? write_t<f16, 128>(a, grid, st) : write_t<f16, 64>(a, grid, st);
+  return 0;
+}
+
+int launch_cache4_read(int fp32, int hd, const C4RowsArgs& a, hipStream_t st) {
+  const dim3 grid = rows_grid(hd, a);
+  if (fp32) {
+    if (hd == 128) cache4_read_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+    else cache4_read_kernel<float, 64><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (hd == 128) cache4_read_kernel<f16, 128><<<grid, 256, 0, st>>>(a);
+    else cache4_read_kernel<f16, 64><<<grid, 256, 0, st>>>(a);
+  }
+  return 0;
+}

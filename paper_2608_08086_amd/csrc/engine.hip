@@ -19,16 +19,19 @@
 
 #include "archer.h"
 #include "archer_ops.h"
+#include "errors.h"
 #include "launch.h"
 
-namespace {
+static thread_local std::string g_err;
 
-thread_local std::string g_err;
-
-archer_status fail(archer_status s, const std::string& msg) {
+archer_status archer_fail(archer_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
+
+namespace {
+
+archer_status fail(archer_status s, const std::string& msg) { return archer_fail(s, msg); }
 
 #define HIPCHK(x)                                                                           \
   do {                                                                                      \
