@@ -508,22 +508,25 @@ def _refuse(status, msg):
     raise ArcherError(status, msg)
 
 
-def _dev(t, dtype, name, strided=False):
-    """Device pointer of a tensor that the call reads or writes on the current device."""
+def _dev(t, dtype, name, dev, strided=False):
+    """Address of a tensor that a call on device `dev` reads or writes."""
     if t.dtype != dtype:
         _refuse(E_ARG, f"{name} must be {dtype}")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         _refuse(E_ARG, f"{name} must be on the current CUDA device")
     if not strided and not t.is_contiguous():
         _refuse(E_ARG, f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _i32(t, n, name):
-    p = _dev(t, torch.int32, name)
+def _i32(t, n, name, dev):
     if t.numel() != n:
         _refuse(E_SHAPE, f"{name} must have {n} elements")
-    return p
+    return _dev(t, torch.int32, name, dev)
+
+
+# the current stream of a device as an address (a torch.cuda.Stream object takes 3 us to make)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 class Cache4:
@@ -535,8 +538,10 @@ class Cache4:
         self.data = data
         self.n_pages, self.n_kv_heads, page_bytes = data.shape
         self.page_size, self.head_dim = page_size, head_dim
-        self.desc = Cache4Desc(_dev(data, torch.uint8, "data"), self.n_pages, page_size, self.n_kv_heads, head_dim)
-        n = lib.archer_cache4_bytes(C.byref(self.desc))
+        self.desc = Cache4Desc(_dev(data, torch.uint8, "data", torch.cuda.current_device()), self.n_pages, page_size,
+                               self.n_kv_heads, head_dim)
+        self.ref = C.byref(self.desc)
+        n = lib.archer_cache4_bytes(self.ref)
         if n == 0:
             _refuse(E_SHAPE, lib.archer_last_error().decode())
         if n != data.numel():
@@ -552,17 +557,19 @@ class Cache4:
 def cache4_plan(len_old, len_new, page_size, table, free_pages, pool, slot_rows):
     """archer_cache4_plan: table [B][max_pages] and free_pages [n_pages] change in place; returns the new
     pool [2], row_off [B + 1], slot_map [slot_rows] and status [1] (int32 tensors; nothing synchronises)."""
-    B = len_old.numel()
+    B, dev = len_old.numel(), torch.cuda.current_device()
     if table.dim() != 2 or table.shape[0] != B:
         _refuse(E_SHAPE, "table must be [batch][max_pages]")
     n_pages, width = free_pages.numel(), table.shape[1]
-    dev = dict(dtype=torch.int32, device=len_old.device)
-    pool_out, status = torch.empty(2, **dev), torch.empty(1, **dev)
-    row_off, slot_map = torch.empty(B + 1, **dev), torch.empty(max(slot_rows, 0), **dev)
-    _check(lib.archer_cache4_plan(B, _i32(len_old, B, "len_old"), _i32(len_new, B, "len_new"), page_size, n_pages, width,
-                                  _i32(table, B * width, "table"), _i32(free_pages, n_pages, "free_pages"),
-                                  _i32(pool, 2, "pool"), pool_out.data_ptr(), row_off.data_ptr(), slot_map.data_ptr(),
-                                  slot_rows, status.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    ptrs = (_i32(len_old, B, "len_old", dev), _i32(len_new, B, "len_new", dev))
+    rows = max(slot_rows, 0)
+    out = torch.empty(rows + B + 4, dtype=torch.int32, device=len_old.device)
+    p = out.data_ptr()
+    slot_map, row_off, pool_out, status = out.split((rows, B + 1, 2, 1))
+    _check(lib.archer_cache4_plan(B, *ptrs, page_size, n_pages, width, _i32(table, B * width, "table", dev),
+                                  _i32(free_pages, n_pages, "free_pages", dev), _i32(pool, 2, "pool", dev),
+                                  p + 4 * (rows + B + 1), p + 4 * rows, p, slot_rows, p + 4 * (rows + B + 3),
+                                  _raw_stream(dev)))
     return pool_out, row_off, slot_map, status
 
 
@@ -577,7 +584,7 @@ def _cache4_dtype(t, name):
 def cache4_write(cache, K, V, slot_map):
     """archer_cache4_write: K, V [n_kv_heads][rows][head_dim] (views; K with unit stride along the last
     dimension, V along the last or the row dimension) into the slots slot_map [rows]."""
-    dt = _cache4_dtype(K.dtype, "K")
+    dt, dev = _cache4_dtype(K.dtype, "K"), torch.cuda.current_device()
     rows = slot_map.numel()
     shape = (cache.n_kv_heads, rows, cache.head_dim)
     if K.shape != shape or V.shape != shape:
@@ -585,19 +592,20 @@ def cache4_write(cache, K, V, slot_map):
     (kh, kr, kd), (vh, vr, vd) = K.stride(), V.stride()
     if kd != 1:
         _refuse(E_UNSUPPORTED, "K must have unit stride along its dimensions")
-    _check(lib.archer_cache4_write(dt, C.byref(cache.desc), rows, _dev(K, K.dtype, "K", True), kh, kr,
-                                   _dev(V, K.dtype, "V", True), vh, vr, vd, _i32(slot_map, rows, "slot_map"),
-                                   torch.cuda.current_stream().cuda_stream))
+    _dev(cache.data, torch.uint8, "the cache", dev)
+    _check(lib.archer_cache4_write(dt, cache.ref, rows, _dev(K, K.dtype, "K", dev, True), kh, kr,
+                                   _dev(V, K.dtype, "V", dev, True), vh, vr, vd, _i32(slot_map, rows, "slot_map", dev),
+                                   _raw_stream(dev)))
 
 
 def cache4_read(cache, slot_map, dtype=torch.float16):
     """archer_cache4_read: the stored rows of slot_map, K and V [n_kv_heads][rows][head_dim]."""
-    dt = _cache4_dtype(dtype, "dtype")
+    dt, dev = _cache4_dtype(dtype, "dtype"), torch.cuda.current_device()
     rows = slot_map.numel()
-    K = torch.empty(cache.n_kv_heads, rows, cache.head_dim, dtype=dtype, device=cache.data.device)
-    V = torch.empty_like(K)
-    _check(lib.archer_cache4_read(dt, C.byref(cache.desc), rows, _i32(slot_map, rows, "slot_map"), K.data_ptr(),
-                                  V.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    _dev(cache.data, torch.uint8, "the cache", dev)
+    K, V = torch.empty(2, cache.n_kv_heads, rows, cache.head_dim, dtype=dtype, device=cache.data.device).unbind()
+    _check(lib.archer_cache4_read(dt, cache.ref, rows, _i32(slot_map, rows, "slot_map", dev), K.data_ptr(), V.data_ptr(),
+                                  _raw_stream(dev)))
     return K, V
 
 
@@ -605,7 +613,8 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
     """archer_op_attention_cache4: Q [Hq][B G][hd] (fp16: O bf16; fp32: O fp32), table [B][max_pages], cached_len [B],
     optional fresh K2 [Hkv][ld2][hd] and Vt2 [Hkv][hd][ld2], optional resp_len [B].  Returns O [B G][Hq hd]
     (preallocated if given: rows past resp_len are not written)."""
-    dt = _cache4_dtype(Q.dtype, "Q")
+    dt, dev = _cache4_dtype(Q.dtype, "Q"), torch.cuda.current_device()
+    _dev(cache.data, torch.uint8, "the cache", dev)
     if Q.dim() != 3 or table.dim() != 2:
         _refuse(E_SHAPE, "Q must be [Hq][B G][hd], table [B][max_pages]")
     (Hq, rows, hd), (B, width) = Q.shape, table.shape
@@ -620,7 +629,7 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
         ld2 = K2.shape[1]
         if K2.shape != (Hkv, ld2, hd) or Vt2.shape != (Hkv, hd, ld2):
             _refuse(E_SHAPE, "K2 must be [Hkv][ld2][hd] and Vt2 [Hkv][hd][ld2]")
-        k2, v2 = _dev(K2, Q.dtype, "K2"), _dev(Vt2, Q.dtype, "Vt2")
+        k2, v2 = _dev(K2, Q.dtype, "K2", dev), _dev(Vt2, Q.dtype, "Vt2", dev)
     otype = torch_dtype(dt)
     if O is None:
         O = torch.empty(rows, Hq * hd, dtype=otype, device=Q.device)
@@ -628,10 +637,10 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
         _refuse(E_SHAPE, "O must be [B G][Hq hd]")
     nbytes = lib.archer_op_attention_cache4_ws_bytes(dt, B, G, Hq, Hkv, hd, max_cached, int(k2 is not None))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
-    _check(lib.archer_op_attention_cache4(dt, C.byref(cache.desc), B, G, Hq, _dev(Q, Q.dtype, "Q"),
-                                          _i32(table, B * width, "table"), width, _i32(cached_len, B, "cached_len"),
-                                          max_cached, k2, v2, ld2, fresh_stride,
-                                          None if resp_len is None else _i32(resp_len, B, "resp_len"),
-                                          _dev(O, otype, "O"), ws.data_ptr() if nbytes else None, nbytes,
-                                          torch.cuda.current_stream().cuda_stream))
+    _check(lib.archer_op_attention_cache4(dt, cache.ref, B, G, Hq, _dev(Q, Q.dtype, "Q", dev),
+                                          _i32(table, B * width, "table", dev), width,
+                                          _i32(cached_len, B, "cached_len", dev), max_cached, k2, v2, ld2, fresh_stride,
+                                          None if resp_len is None else _i32(resp_len, B, "resp_len", dev),
+                                          _dev(O, otype, "O", dev), ws.data_ptr() if nbytes else None, nbytes,
+                                          _raw_stream(dev)))
     return O
