@@ -133,14 +133,16 @@ def read(data, page_size, hd, slots):
 # -- attention -----------------------------------------------------------------------------------
 def attention(Q, K, V):
     """Q [M][hd], K, V [n][hd] -> O [M][hd] and, for error bounds, A = sum p |v| / sum p, the largest
-    sum |q k| / sqrt(hd) and the largest score magnitude (zeros without keys)."""
+    sum |q k| / sqrt(hd) with each q taken as its 32 dimensions' largest, and the largest score magnitude
+    (zeros without keys)."""
     M, hd = Q.shape
     if len(K) == 0:
         return np.zeros((M, hd)), np.zeros((M, hd)), 0.0, 0.0
     s = Q @ K.T / np.sqrt(hd)
     p = np.exp(s - s.max(-1, keepdims=True))
     p /= p.sum(-1, keepdims=True)
-    return p @ V, p @ np.abs(V), float((np.abs(Q) @ np.abs(K).T).max() / np.sqrt(hd)), float(np.abs(s).max())
+    top = np.repeat(np.abs(Q).reshape(M, hd // BLOCK, BLOCK).max(-1), BLOCK, axis=-1)
+    return p @ V, p @ np.abs(V), float((top @ np.abs(K).T).max() / np.sqrt(hd)), float(np.abs(s).max())
 
 
 def attention_bound(O, A, qk, smax, n, hd, vmax, half):
@@ -148,11 +150,15 @@ def attention_bound(O, A, qk, smax, n, hd, vmax, half):
 
     A score is a sum of hd products in fp32, each rounding at most 2^-24 of the running sum of magnitudes,
     then scaled and rounded: (hd + 3) 2^-24 qk, and 2^-23 smax for the exponent's argument.  The exponential
-    itself: 2^-22.  These are relative errors of the probabilities, in the numerator and in the denominator.
+    itself: 2^-22.  With fp16 queries the row kernel multiplies three e2m3 terms of each query element: the
+    first is off by at most 2^-2 of its scale s1 (half the largest step), the second, of scale s1 / 16 and at
+    most 4 of it, by 2^-3 s1 / 16, the third, of scale s1 / 512, by 2^-3 s1 / 512 = 2^-12 s1; s1 is the least power of two that
+    has the block's largest element below 7.5 s1, which therefore exceeds 3.75 s1: 2^-13.9 of it, 2^-13.9 qk in
+    a score.  These are relative errors of the probabilities, in the numerator and in the denominator.
     Sums over n keys in fp32, with one rescale per 32 keys: (n + n / 16 + 40) 2^-24 in both.  fp16 probabilities:
-    half a step is 2^-11 relative, and 2^-25 absolute where they are subnormal (the largest is 1, so that the
-    denominator is at least 1).  The output's own rounding: bf16 2^-8, fp32 2^-24."""
-    rel = 2 * ((hd + 3) * 2.0**-24 * qk + 2.0**-23 * smax + 2.0**-22 + (n + n / 16 + 40) * 2.0**-24)
+    half a step is 2^-11 relative, and 2^-25 absolute where they are subnormal (the largest is between 1 and
+    2^8, so that the denominator is at least 1).  The output's own rounding: bf16 2^-8, fp32 2^-24."""
+    rel = 2 * (((hd + 3) * 2.0**-24 + half * 2.0**-13.9) * qk + 2.0**-23 * smax + 2.0**-22 + (n + n / 16 + 40) * 2.0**-24)
     if not half:
         return 2.0**-24 * np.abs(O) + A * rel + 1e-30
     return 2.0**-8 * np.abs(O) + A * (rel + 2.0**-11) + n * 2.0**-25 * vmax + 1e-30

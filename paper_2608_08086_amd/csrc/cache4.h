@@ -72,15 +72,20 @@ struct Attn4Args {
   int ld2, fstride;
   const int* resp_len;          // or null
   void* O;                      // [batch * G][hq * hd]
-  float *Opart, *ML;            // split partials [split][batch * G][hq][hd], [split][batch * G][hq][2]
+  float *Opart, *ML;            // chunk partials [slots][hkv][G * hq / hkv][hd], and (m, l) of each
   int batch, G, hq, hkv, hd;
-  int nsplit, chunk_min;        // splits of a sequence's steps: at most nsplit, of at least chunk_min steps
+  int target, chunk_min, slots, step; // see Attn4Split
   float scale_log2;
+};
+
+// How a call's keys are cut, from what the host knows of it: chunks of
+// max(all steps / target, chunk_min) steps, at most `slots` of them (target 0: one per sequence).
+struct Attn4Split {
+  int target, chunk_min, slots, step;   // step: keys of a step
 };
 
 void launch_cache4_plan(const C4PlanArgs& a, hipStream_t st);
 int launch_cache4_write(int fp32, int hd, const C4RowsArgs& a, hipStream_t st);
 int launch_cache4_read(int fp32, int hd, const C4RowsArgs& a, hipStream_t st);
-// The splits of an attention call, from what the host knows of it.
-int attn4_splits(int fp32, int batch, int G, int hq, int hkv, int max_cached, int fresh);
+Attn4Split attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh);
 int launch_attn4(int fp32, const Attn4Args& a, hipStream_t st);

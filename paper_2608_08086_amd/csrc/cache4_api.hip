@@ -135,9 +135,9 @@ size_t archer_op_attention_cache4_ws_bytes(int32_t dtype, int32_t batch, int32_t
   if ((dtype != ARCHER_BF16 && dtype != ARCHER_FP32) || batch < 1 || G < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || hd < 1 ||
       max_cached < 0)
     return 0;
-  const size_t ns = attn4_splits(dtype == ARCHER_FP32, batch, G, Hq, Hkv, max_cached, fresh);
-  if (ns == 1) return 0;
-  const size_t rows = ns * batch * G * Hq;
+  const Attn4Split s = attn4_split(dtype == ARCHER_FP32, batch, G, Hq, Hkv, hd, max_cached, fresh);
+  if (s.slots == batch) return 0;
+  const size_t rows = (size_t)s.slots * G * Hq;
   return align_up(rows * hd * 4, 256) + align_up(rows * 2 * 4, 256);
 }
 
@@ -169,15 +169,15 @@ archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4* cac
   a.K2 = K2; a.Vt2 = Vt2; a.ld2 = ld2; a.fstride = fresh_stride; a.resp_len = resp_len;
   a.O = O;
   a.batch = batch; a.G = G; a.hq = Hq; a.hkv = hkv; a.hd = hd;
-  a.nsplit = attn4_splits(fp32, batch, G, Hq, hkv, max_cached, K2 != nullptr);
-  a.chunk_min = 1;
+  const Attn4Split sp = attn4_split(fp32, batch, G, Hq, hkv, hd, max_cached, K2 != nullptr);
+  a.target = sp.target; a.chunk_min = sp.chunk_min; a.slots = sp.slots; a.step = sp.step;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
-  if (a.nsplit > 1) {
+  if (a.slots > batch) {
     if (!workspace || ((uintptr_t)workspace & 255) ||
         ws_bytes < archer_op_attention_cache4_ws_bytes(dtype, batch, G, Hq, hkv, hd, max_cached, K2 != nullptr))
       return archer_fail(ARCHER_E_WORKSPACE, "attention workspace too small or misaligned");
     a.Opart = (float*)workspace;
-    a.ML = (float*)((char*)workspace + align_up((size_t)a.nsplit * batch * G * Hq * hd * 4, 256));
+    a.ML = (float*)((char*)workspace + align_up((size_t)a.slots * G * Hq * hd * 4, 256));
   }
   if (launch_attn4(fp32, a, (hipStream_t)hip_stream)) return archer_fail(ARCHER_E_UNSUPPORTED, "attention shape unsupported");
   HIPCHK(hipGetLastError());

@@ -362,6 +362,79 @@ def test_same_bits_again_and_on_another_stream(dtype, G):
     assert torch.equal(a, b)
 
 
+# -- columns enough for the whole GPU: 2^15 of 128 dimensions, 2^16 of 64 -------------------------
+SOME = np.r_[0, 1, 15:18, 31, 32, 63, 64, np.arange(97, 1024, 101), 127, 128, 255, 511]
+
+
+@pytest.mark.parametrize("lens,G,hq,hkv,hd,page,fresh,resp", [
+    # a workgroup's waves all in use, some, and in the second one few
+    ([0, 1, 63, 64, 65, 130, 257, 700], 512, 8, 8, 128, 32, True, [512, 1, 0, 33, 300, 512, 257, 100]),
+    ([191, 192, 193, 0] * 4, 160, 14, 2, 128, 64, False, None),
+    (list(range(41)), 100, 8, 8, 128, 256, True, None),
+    ([2100, 40, 0, 1], 1024, 8, 8, 128, 128, True, [1024, 1000, 1024, 7]),       # more than 32 tiles
+    ([0] * 8, 512, 8, 8, 128, 32, False, None),
+    ([0, 31, 33, 70, 200, 1, 64, 9] * 2, 256, 16, 4, 64, 32, True, [256, 255, 0, 1, 17, 128, 200, 64] * 2),
+    ([500, 20, 0, 300] * 4, 512, 8, 8, 64, 256, False, None),
+])
+def test_wide_attention_matches_oracle(lens, G, hq, hkv, hd, page, fresh, resp):
+    say(f"wide attention lens={lens} G={G} hq={hq} hkv={hkv} hd={hd} page={page} fresh={fresh}")
+    c = Case(F16, lens, G, hq, hkv, hd, page, fresh, resp, seed=30 + hd)
+    say(f"  worst error / bound {c.check(c.run(), rows_of=SOME):.3f}")
+
+
+WIDE = [(8, 4, 128), (16, 8, 64)]       # hq, hkv, hd; of 8 sequences and 512 rows
+WIDE_LENS = [300, 41, 0, 90, 64, 128, 7, 200]
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDE)
+def test_wide_peaked_scores(hq, hkv, hd):
+    c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 32, True, seed=31, q_scale=30.0)
+    c.check(c.run(), rows_of=SOME)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDE)
+def test_wide_bad_pages_and_max_cached(hq, hkv, hd):
+    c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 64, False, seed=32, share=True)
+    c.check(c.run(max_cached=5000), rows_of=SOME)
+    t = c.table.copy()
+    t[0, 1], t[0, 4], t[1, 0] = len(c.data), -1, 2**31 - 1
+    K, V = list(c.K), list(c.V)
+    keep = np.r_[0:64, 128:256]
+    c.K[0], c.V[0], c.K[1], c.V[1] = K[0][:, keep], V[0][:, keep], K[1][:, :0], V[1][:, :0]
+    c.check(c.run(table=t), rows_of=SOME)
+    # a bound below some lengths
+    c.K, c.V = [k[:, :100] for k in K], [v[:, :100] for v in V]
+    c.check(c.run(max_cached=100), rows_of=SOME)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDE)
+def test_wide_nan_and_infinity_stay_in_place(hq, hkv, hd):
+    c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 64, True, seed=33)
+    ref = host(c.run()).reshape(8, 512, hq, hd)
+    page, pos = divmod(77, 64)
+    data = c.data.copy()
+    data[c.table[0, page], 1, oc.locate(64, hd)[3][pos, 1]] = oc.NAN_SCALE
+    c.Q[1, 3 * 512 + 5, 9] = np.inf                # sequence 3, row 5, head 1
+    c.Q[0, 3 * 512 + 6, 0] = np.nan
+    got = host(c.run(data=data)).reshape(8, 512, hq, hd)
+    want = np.zeros(got.shape[:3], bool)
+    want[0, :, 2:4] = want[3, 5, 1] = want[3, 6, 0] = True
+    assert np.isnan(got[want]).all()
+    np.testing.assert_array_equal(got[~want], ref[~want])
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDE)
+def test_wide_same_bits_again_and_on_another_stream(hq, hkv, hd):
+    c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 64, True, seed=34)
+    a = c.run()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        b = c.run()
+    s.synchronize()
+    assert torch.equal(a, b)
+
+
 # -- as they are used ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype,hq,hkv,hd,page", [(F16, 4, 2, 128, 32), (F32, 2, 2, 64, 64)])
 def test_plan_store_attend_rollback(dtype, hq, hkv, hd, page):
