@@ -154,6 +154,16 @@ void launch_cache4_plan(const C4PlanArgs& a, hipStream_t st) {
 // 16-byte loads (row-major: 8 dimensions of one row; transposed: 8 rows of one dimension).
 // The four threads of a scale block share a row quad (row-major) or the four
 // 16-lane groups of a wave (transposed).
+//
+// Rows are stored in eights that begin where the cache's 8-token blocks do, so that a
+// ragged batch is stored 32 bytes of values at a time, not 4, but for the ends of its sequences.
+// Row-major: workgroup k takes the rows from
+//   cut(k) = R - slot[R] mod 8,  R = k STEP,
+// any choice of which is a partition, and the slots of a prompt that runs through R
+// make it the beginning of a block; a workgroup has 8 rows more than STEP for that.
+// Transposed: rows in the order of the source's 16-byte pieces, or its loads would straddle lines
+// (16 prompts of 1344 rows, 32 heads of 128 dimensions, from the third token of a block: 113 us
+// that way), and regrouped in LDS.
 __device__ __forceinline__ unsigned quad_max_u32(unsigned v) {
   v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true));   // lanes xor 1
   return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true));   // lanes xor 2
@@ -165,61 +175,34 @@ __device__ __forceinline__ unsigned group_max_u32(unsigned v) {
   return max((unsigned)b[0], (unsigned)b[1]);
 }
 
-// 8 consecutive elements in fp32, n of them readable; vec: 16-byte loads are allowed
-template <class T>
-__device__ __forceinline__ void load8(const T* p, long step, int n, bool vec, float* x) {
-  if (vec && n == 8) {
-    if constexpr (sizeof(T) == 2) {
-      const f16x8 v = __builtin_bit_cast(f16x8, *(const u32x4*)p);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-    } else {
-      const f32x4 v = *(const f32x4*)p, u = *(const f32x4*)(p + 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { x[e] = v[e]; x[4 + e] = u[e]; }
-    }
-    return;
+// 8 consecutive elements
+template <class T> struct Eight;
+template <> struct Eight<f16> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const f16* p) { __builtin_memcpy(&v, p, 16); }
+  __device__ __forceinline__ float get(int e) const { return (float)__builtin_bit_cast(f16x8, v)[e]; }
+  __device__ __forceinline__ void set(int e, f16 x) {
+    f16x8 y = __builtin_bit_cast(f16x8, v);
+    y[e] = x;
+    v = __builtin_bit_cast(u32x4, y);
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = e < n ? to_f32(p[e * step]) : 0.f;
-}
+};
+template <> struct Eight<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(v, p, 32); }
+  __device__ __forceinline__ float get(int e) const { return v[e >> 2][e & 3]; }
+  __device__ __forceinline__ void set(int e, float x) { v[e >> 2][e & 3] = x; }
+};
 
-template <class T, int HD, bool TRANS>
-__device__ __forceinline__ void cache4_store(const C4RowsArgs& a, const T* src, long s_row, long s_dim, bool vec,
-                                             bool value) {
-  constexpr int U = HD / 8;                        // threads across a row
-  const int tid = threadIdx.x, h = blockIdx.y;
-  const int unit = TRANS ? (tid >> 4) % U : tid % U;
-  const int oct = TRANS ? (tid & 15) + 16 * ((tid >> 4) / U) : tid / U;
-  const long r0 = ((long)blockIdx.x * (256 / U) + oct) * 8;
-  // threads past the last row stay for the reductions
-  const int n = (int)min(8L, max(0L, a.rows - r0));
-  int slot[8];
-  const long nslots = (long)a.c.n_pages << a.c.psh;
-  bool run = n == 8;
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    slot[r] = r < n ? a.slots[r0 + r] : -1;
-    if (slot[r] < 0 || slot[r] >= nslots) slot[r] = -1;
-    run = run && slot[r] == slot[0] + r;
-  }
-  run = run && slot[0] >= 0 && (slot[0] & 7) == 0;   // an aligned 8-token block
+template <int HD> struct WriteRows {
+  static constexpr int U = HD / 8;                 // threads across a row
+  static constexpr int ALL = 256 / U * 8;          // rows that a workgroup's threads own
+  static constexpr int STEP = ALL - 8;             // rows of a row-major workgroup, but for the cuts
+};
 
-  float x[8][8];                                   // [row][dimension]
-  if constexpr (TRANS) {
-#pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      float t[8];
-      load8(src + (unit * 8 + d) * s_dim + r0, 1, n, vec, t);
-#pragma unroll
-      for (int r = 0; r < 8; ++r) x[r][d] = t[r];
-    }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 8; ++r) load8(src + (r0 + r) * s_row + unit * 8 * s_dim, s_dim, r < n ? 8 : 0, vec, x[r]);
-  }
-
-  unsigned code[8], eb[8];
+// Codes and scale bytes of 8 rows of this thread's 8 dimensions.
+template <bool TRANS>
+__device__ __forceinline__ void quantise(const float (&x)[8][8], unsigned (&code)[8], unsigned (&eb)[8]) {
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     unsigned top = 0;                              // |x| as integers: NaN above infinity above the rest
@@ -238,12 +221,25 @@ __device__ __forceinline__ void cache4_store(const C4RowsArgs& a, const T* src, 
     code[r] = c;
     eb[r] = top > 0x7f800000u ? (unsigned)C4_NAN : e;
   }
+}
+
+// Stores the first n rows at their slots: dimensions 8 unit ...; a scale by the first of its four threads.
+template <int HD>
+__device__ __forceinline__ void store_rows(const C4RowsArgs& a, bool value, int unit, int n, int (&slot)[8],
+                                           const unsigned (&code)[8], const unsigned (&eb)[8]) {
+  const long nslots = (long)a.c.n_pages << a.c.psh;
+  bool run = n == 8;                               // the rows fill an aligned 8-token block
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    slot[r] = ((r < n) & (slot[r] < nslots)) ? slot[r] : -1;
+    run &= slot[r] == slot[0] + r;
+  }
+  run &= (slot[0] >= 0) & ((slot[0] & 7) == 0);
 
   using L = C4<HD>;
-  const int T_ = 1 << a.c.psh;
+  const int T_ = 1 << a.c.psh, h = blockIdx.y, g = unit >> 2;
   const size_t pb = L::page_bytes(T_);
-  const bool first = (unit & 3) == 0;              // the thread that stores the block's scale
-  const int g = unit >> 2;
+  const bool first = (unit & 3) == 0;
   if (run) {
     const int t0 = slot[0] & (T_ - 1);
     uint8_t* page = a.c.data + ((size_t)(slot[0] >> a.c.psh) * a.c.hkv + h) * pb;
@@ -290,21 +286,109 @@ __device__ __forceinline__ void cache4_store(const C4RowsArgs& a, const T* src, 
   }
 }
 
-template <class T>
-__device__ __forceinline__ bool aligned16(const void* p, long a, long b) {
-  return (((uintptr_t)p | (uintptr_t)(a * (long)sizeof(T)) | (uintptr_t)(b * (long)sizeof(T))) & 15) == 0;
+// In both: every load is requested before the first of them is looked at (a branch around each
+// waits for each).  Rows past the last one read that one, and are not stored.
+
+// src: a head's rows, s_row apart
+template <class T, int HD>
+__device__ __forceinline__ void write_rows(const C4RowsArgs& a, const T* src, long s_row, bool value) {
+  using W = WriteRows<HD>;
+  const int tid = threadIdx.x, unit = tid % W::U;
+  auto cut = [&](long k) __attribute__((always_inline)) {
+    const long R = k * W::STEP;
+    return R >= a.rows ? (long)a.rows : k ? R - (a.slots[R] & 7) : 0;
+  };
+  const long r0 = cut(blockIdx.x) + tid / W::U * 8, r1 = cut(blockIdx.x + 1L);
+  int slot[8];
+  Eight<T> t[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) t[r].load(src + min(r0 + r, (long)a.rows - 1) * s_row + unit * 8);
+#pragma unroll
+  for (int r = 0; r < 8; ++r) slot[r] = a.slots[min(r0 + r, (long)a.rows - 1)];
+  float x[8][8];                                   // [row][dimension]
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+#pragma unroll
+    for (int d = 0; d < 8; ++d) x[r][d] = t[r].get(d);
+  unsigned code[8], eb[8];
+  quantise<false>(x, code, eb);                    // by all threads: it exchanges maxima
+  store_rows<HD>(a, value, unit, (int)min(8L, max(0L, r1 - r0)), slot, code, eb);
+}
+
+// src: a head's values, dimensions s_dim apart, rows one element
+template <class T, int HD>
+__device__ __forceinline__ void write_transposed(const C4RowsArgs& a, const T* src, long s_dim) {
+  using W = WriteRows<HD>;
+  constexpr int U = W::U, OCT = 8 * U + 4;         // an eight's words in LDS: 16 eights 4 banks apart
+  __shared__ unsigned codes[W::ALL / 8 * OCT];
+  __shared__ __attribute__((aligned(8))) uint8_t scales[U / 4][W::ALL];
+  const int tid = threadIdx.x;
+  const long b0 = (long)blockIdx.x * W::ALL;
+  const int nrows = (int)min((long)W::ALL, a.rows - b0);      // of this workgroup, at least 1
+  // where the workgroup's eights begin, and the slots of this thread's
+  const int unit = tid % U, lead = a.slots[b0] & 7, q0 = tid / U * 8 - lead;
+  int slot[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) slot[r] = a.slots[b0 + min(max(q0 + r, 0), nrows - 1)];
+  {
+    const int u = (tid >> 4) % U, oct = (tid & 15) + 16 * ((tid >> 4) / U);
+    Eight<T> t[8];
+    if (oct * 8 + 8 <= nrows) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) t[d].load(src + (u * 8 + d) * s_dim + b0 + oct * 8);
+    } else {
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) t[d].set(r, src[(u * 8 + d) * s_dim + b0 + min(oct * 8 + r, nrows - 1)]);
+      asm volatile("" ::: "memory");               // or the other branch's loads are taken apart to share these
+    }
+    float x[8][8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int d = 0; d < 8; ++d) x[r][d] = t[d].get(r);
+    unsigned code[8], eb[8];
+    quantise<true>(x, code, eb);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) codes[oct * OCT + r * U + u] = code[r];
+    if ((u & 3) == 0) {
+      u32x2 s = {eb[0] | eb[1] << 8 | eb[2] << 16 | eb[3] << 24, eb[4] | eb[5] << 8 | eb[6] << 16 | eb[7] << 24};
+      *(u32x2*)&scales[u >> 2][oct * 8] = s;
+    }
+  }
+  __syncthreads();
+  // the eight of rows q .. q + 7, of which those inside the workgroup's are stored
+  auto put = [&](int q) __attribute__((always_inline)) {
+    const int s0 = max(q, 0), n = min(q + 8, nrows) - s0;
+    unsigned code[8], eb[8];
+    int at[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      // a first eight that begins before the workgroup: its rows moved to the front
+      const int k = min(s0 + r, W::ALL - 1);
+      code[r] = codes[(k >> 3) * OCT + (k & 7) * U + unit];
+      eb[r] = scales[unit >> 2][k];
+      at[r] = slot[r];
+    }
+    store_rows<HD>(a, true, unit, n, at, code, eb);
+  };
+  if (q0 < 0) {                                    // its slots, moved likewise; and the rows behind the last eight
+#pragma unroll
+    for (int r = 0; r < 8; ++r) slot[r] = a.slots[b0 + min(W::ALL - lead + r, nrows - 1)];
+    put(W::ALL - lead);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) slot[r] = a.slots[b0 + min(r, nrows - 1)];
+  }
+  put(q0);
 }
 
 template <class T, int HD, bool VT>
 __global__ __launch_bounds__(256) void cache4_write_kernel(C4RowsArgs a) {
   const int h = blockIdx.y;
-  if (blockIdx.z == 0) {
-    cache4_store<T, HD, false>(a, (const T*)a.K + h * a.k_head, a.k_row, 1, aligned16<T>(a.K, a.k_head, a.k_row), false);
-  } else if constexpr (VT) {
-    cache4_store<T, HD, true>(a, (const T*)a.V + h * a.v_head, 1, a.v_dim, aligned16<T>(a.V, a.v_head, a.v_dim), true);
-  } else {
-    cache4_store<T, HD, false>(a, (const T*)a.V + h * a.v_head, a.v_row, 1, aligned16<T>(a.V, a.v_head, a.v_row), true);
-  }
+  if (blockIdx.z == 0) write_rows<T, HD>(a, (const T*)a.K + h * a.k_head, a.k_row, false);
+  else if constexpr (!VT) write_rows<T, HD>(a, (const T*)a.V + h * a.v_head, a.v_row, true);
+  else if ((long)blockIdx.x * WriteRows<HD>::ALL < a.rows) write_transposed<T, HD>(a, (const T*)a.V + h * a.v_head, a.v_dim);
 }
 
 // Read back: the same thread-to-row map (row-major), each row's 8 dimensions
@@ -321,35 +405,43 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(C4RowsArgs a) {
   const size_t pb = L::page_bytes(T_);
   const long nslots = (long)a.c.n_pages << a.c.psh;
   T* out = (T*)(value ? a.Vo : a.Ko) + ((size_t)h * a.rows + r0) * HD + unit * 8;
+  // every slot, then every row's bytes, is requested before the first is used;
+  // a slot outside the cache reads the first one, times zero
+  int slot[8];
+  unsigned c[8], e[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) slot[r] = a.slots[min(r0 + r, (long)a.rows - 1)];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const bool ok = slot[r] >= 0 && slot[r] < nslots;
+    const int at = ok ? slot[r] : 0, t = at & (T_ - 1);
+    const uint8_t* page = a.c.data + ((size_t)(at >> a.c.psh) * a.c.hkv + h) * pb;
+    if (!value) {
+      c[r] = *(const unsigned*)(page + (size_t)t * L::KROW + unit * 4);
+    } else if constexpr (HD == 128) {
+      c[r] = *(const unsigned*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 4);
+    } else {
+      const uint16_t* p = (const uint16_t*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 2);
+      c[r] = p[0] | (unsigned)p[8] << 16;
+    }
+    e[r] = page[(value ? L::vsoff(T_) : L::ksoff(T_)) + (t >> 3) * L::SBLK + g * 8 + (t & 7)];
+    slot[r] = ok;
+  }
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     if (r >= n) break;
-    const int slot = a.slots[r0 + r];
-    unsigned c = 0, e = 0;
-    if (slot >= 0 && slot < nslots) {
-      const int t = slot & (T_ - 1);
-      const uint8_t* page = a.c.data + ((size_t)(slot >> a.c.psh) * a.c.hkv + h) * pb;
-      if (!value) {
-        c = *(const unsigned*)(page + (size_t)t * L::KROW + unit * 4);
-      } else if constexpr (HD == 128) {
-        c = *(const unsigned*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 4);
-      } else {
-        const uint16_t* p = (const uint16_t*)(page + L::voff(T_) + (t >> 3) * L::VBLK + unit * 32 + (t & 7) * 2);
-        c = p[0] | (unsigned)p[8] << 16;
-      }
-      e = page[(value ? L::vsoff(T_) : L::ksoff(T_)) + (t >> 3) * L::SBLK + g * 8 + (t & 7)];
-    }
-    const float sc = __uint_as_float(e << 23);     // 255: every element NaN
+    const unsigned w = slot[r] ? c[r] : 0;
+    const float sc = __uint_as_float(slot[r] ? e[r] << 23 : 0);     // 255: every element NaN
     if constexpr (sizeof(T) == 2) {
       u32x4 v;
-      v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 0));
-      v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 1));
-      v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 2));
-      v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, sc, 3));
+      v[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 0));
+      v[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 1));
+      v[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 2));
+      v[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, sc, 3));
       *(u32x4*)(out + (size_t)r * HD) = v;
     } else {
-      const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 1);
-      const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, sc, 3);
+      const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 1);
+      const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 3);
       *(f32x4*)(out + (size_t)r * HD) = f32x4{p0[0], p0[1], p1[0], p1[1]};
       *(f32x4*)(out + (size_t)r * HD + 4) = f32x4{p2[0], p2[1], p3[0], p3[1]};
     }
@@ -357,31 +449,27 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(C4RowsArgs a) {
 }
 
 template <class T, int HD>
-static void write_t(const C4RowsArgs& a, dim3 grid, hipStream_t st) {
+static void write_t(const C4RowsArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((a.rows + (long)WriteRows<HD>::STEP - 1) / WriteRows<HD>::STEP), (unsigned)a.c.hkv, 2);
   if (a.v_dim == 1) cache4_write_kernel<T, HD, false><<<grid, 256, 0, st>>>(a);
   else cache4_write_kernel<T, HD, true><<<grid, 256, 0, st>>>(a);
 }
 
-static dim3 rows_grid(int hd, const C4RowsArgs& a) {
-  const int per = 256 / (hd / 8) * 8;
-  return dim3((unsigned)((a.rows + (long)per - 1) / per), (unsigned)a.c.hkv, 2);
+template <class T, int HD>
+static void read_t(const C4RowsArgs& a, hipStream_t st) {
+  constexpr int per = 256 / (HD / 8) * 8;
+  const dim3 grid((unsigned)((a.rows + (long)per - 1) / per), (unsigned)a.c.hkv, 2);
+  cache4_read_kernel<T, HD><<<grid, 256, 0, st>>>(a);
 }
 
 int launch_cache4_write(int fp32, int hd, const C4RowsArgs& a, hipStream_t st) {
-  const dim3 grid = rows_grid(hd, a);
-  if (fp32) hd == 128 ? write_t<float, 128>(a, grid, st) : write_t<float, 64>(a, grid, st);
-  else hd == 128 ? write_t<f16, 128>(a, grid, st) : write_t<f16, 64>(a, grid, st);
+  if (fp32) hd == 128 ? write_t<float, 128>(a, st) : write_t<float, 64>(a, st);
+  else hd == 128 ? write_t<f16, 128>(a, st) : write_t<f16, 64>(a, st);
   return 0;
 }
 
 int launch_cache4_read(int fp32, int hd, const C4RowsArgs& a, hipStream_t st) {
-  const dim3 grid = rows_grid(hd, a);
-  if (fp32) {
-    if (hd == 128) cache4_read_kernel<float, 128><<<grid, 256, 0, st>>>(a);
-    else cache4_read_kernel<float, 64><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (hd == 128) cache4_read_kernel<f16, 128><<<grid, 256, 0, st>>>(a);
-    else cache4_read_kernel<f16, 64><<<grid, 256, 0, st>>>(a);
-  }
+  if (fp32) hd == 128 ? read_t<float, 128>(a, st) : read_t<float, 64>(a, st);
+  else hd == 128 ? read_t<f16, 128>(a, st) : read_t<f16, 64>(a, st);
   return 0;
 }
