@@ -17,8 +17,11 @@
 // The ring entries read lie in [head, head + count), those written behind
 // them, so no order between workgroups is needed and the call may be repeated
 // with the same result.  Every workgroup makes the sums for itself (a few
-// thousand numbers from L2: 2 us) rather than wait for one that does, and
+// thousand numbers from L2) rather than wait for one that does, and
 // takes the slots from the sums, not from the table that others are writing.
+// Bound by the chain of dependent loads (lengths, then a length and a page per slot) and
+// the launch: 4.6 us for 64 requests that grow by one token, 9.8 us for 1024 of which a
+// quarter gives its pages back and the others grow by up to 2048 (3 MB of slots).
 constexpr int PLAN_THREADS = 256;
 constexpr int PLAN_ROWS = 4;     // slots a thread makes with one search
 
@@ -57,13 +60,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache4_plan_kernel(C4PlanArgs a)
   const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
   // totals in 64 bits: lengths far beyond the table must not wrap into it
   long long st = 0, sg = 0, sr = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int o = a.len_old[b], n = a.len_new[b];
-    if (o < 0 || n < 0 || o > cap || n > cap) bad_len = 1;
-    const int have = (int)(((long long)o + T - 1) >> a.psh), want = (int)(((long long)n + T - 1) >> a.psh);
-    st += max(want - have, 0);
-    sg += max(have - want, 0);
-    sr += max((long long)n - o, 0LL);
+  // four requests' lengths at a time; past the thread's last one, an unchanged length
+  auto four = [&](int b, int* o, int* n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i] = a.len_old[min(b + i, B - 1)];
+      n[i] = a.len_new[min(b + i, B - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (b + i >= b1) o[i] = n[i] = 0;
+  };
+  for (int b = b0; b < b1; b += 4) {
+    int o[4], n[4];
+    four(b, o, n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if ((o[i] < 0) | (n[i] < 0) | (o[i] > cap) | (n[i] > cap)) bad_len = 1;
+      const int have = (int)(((long long)o[i] + T - 1) >> a.psh), want = (int)(((long long)n[i] + T - 1) >> a.psh);
+      st += max(want - have, 0);
+      sg += max(have - want, 0);
+      sr += max((long long)n[i] - o[i], 0LL);
+    }
   }
   const int w = tid >> 6, lane = tid & 63;
   const long long it = wave_scan_i64(st), ig = wave_scan_i64(sg), ir = wave_scan_i64(sr);
@@ -84,51 +102,75 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache4_plan_kernel(C4PlanArgs a)
   else if (tr > a.slot_rows) status = 3;
   const int total = status ? 0 : (int)tr;
   if (!status) {
-    for (int b = b0; b < b1; ++b) {
-      const int o = a.len_old[b], n = a.len_new[b];
-      const int have = (int)(((long long)o + T - 1) >> a.psh), want = (int)(((long long)n + T - 1) >> a.psh);
-      taken[b] = (int)bt; given[b] = (int)bg; rows[b] = (int)br;
-      bt += max(want - have, 0);
-      bg += max(have - want, 0);
-      br += max(n - o, 0);
+    for (int b = b0; b < b1; b += 4) {
+      int o[4], n[4];
+      four(b, o, n);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int have = (int)(((long long)o[i] + T - 1) >> a.psh), want = (int)(((long long)n[i] + T - 1) >> a.psh);
+        if (b + i < b1) taken[b + i] = (int)bt, given[b + i] = (int)bg, rows[b + i] = (int)br;
+        bt += max(want - have, 0);
+        bg += max(have - want, 0);
+        br += max(n[i] - o[i], 0);
+      }
     }
     if (tid == 0) { taken[B] = (int)tt; given[B] = (int)tg; rows[B] = (int)tr; }
   }
   __syncthreads();
 
+  // entry head + i of the ring, 0 <= i <= n_pages as far as the status is 0
+  auto ring = [&](int i) __attribute__((always_inline)) {
+    const unsigned k = (unsigned)head + (unsigned)i, n = (unsigned)a.n_pages;
+    return k >= n ? k - n : k;
+  };
   const int gid = blockIdx.x * PLAN_THREADS + tid, gsz = gridDim.x * PLAN_THREADS;
   if (gid == 0) {
     *a.status = status;
-    a.pool_out[0] = status ? head : (int)(((long long)head + tt) % a.n_pages);
+    a.pool_out[0] = status ? head : (int)ring((int)tt);
     a.pool_out[1] = status ? count : (int)(count - tt + tg);
   }
   for (int b = gid; b <= B; b += gsz) a.row_off[b] = status ? 0 : rows[b];
   if (!status) {
-    for (int r = gid; r < (int)tt; r += gsz) {
+    // from the last thread on, for the first ones have the most to do below
+    for (int r = gsz - 1 - gid; r < (int)tt; r += gsz) {
       const int b = scan_find(taken, B, r);
       const int have = (a.len_old[b] + T - 1) >> a.psh;
-      a.table[(size_t)b * a.width + have + r - taken[b]] = a.free_pages[((long long)head + r) % a.n_pages];
+      a.table[(size_t)b * a.width + have + r - taken[b]] = a.free_pages[ring(r)];
     }
-    for (int r = gid; r < (int)tg; r += gsz) {
+    for (int r = (gid + gsz / 2) % gsz; r < (int)tg; r += gsz) {
       const int b = scan_find(given, B, r);
       const int want = (a.len_new[b] + T - 1) >> a.psh;
-      a.free_pages[((long long)head + count + r) % a.n_pages] = a.table[(size_t)b * a.width + want + r - given[b]];
+      a.free_pages[ring(count + r)] = a.table[(size_t)b * a.width + want + r - given[b]];
     }
   }
+  // All four lengths, then all four pages, are requested before the first is used; rows
+  // past the last one take that one's, and are -1.  (Addresses of the global address space by
+  // name: the compiler would not know them for such after the choice between the two.)
+  typedef const __attribute__((address_space(1))) int* gint;
   for (long long r0 = (long long)gid * PLAN_ROWS; r0 < a.slot_rows; r0 += (long long)gsz * PLAN_ROWS) {
     int s[PLAN_ROWS];
-    int b = r0 < total ? scan_find(rows, B, (int)r0) : 0;
 #pragma unroll
-    for (int e = 0; e < PLAN_ROWS; ++e) {
-      const int r = (int)r0 + e;
-      s[e] = -1;
-      if (r0 + e < total) {
-        while (r >= rows[b + 1]) ++b;              // ends: rows[B] = total > r
-        const int o = a.len_old[b], p = o + r - rows[b], j = p >> a.psh, have = (o + T - 1) >> a.psh;
-        const int page = j < have ? a.table[(size_t)b * a.width + j]
-                                  : a.free_pages[((long long)head + taken[b] + j - have) % a.n_pages];
-        if (page >= 0 && page < a.n_pages) s[e] = (page << a.psh) + (p & (T - 1));
+    for (int e = 0; e < PLAN_ROWS; ++e) s[e] = -1;
+    if (r0 < total) {
+      int b[PLAN_ROWS], r[PLAN_ROWS], o[PLAN_ROWS];
+#pragma unroll
+      for (int e = 0; e < PLAN_ROWS; ++e) {
+        r[e] = (int)min(r0 + e, total - 1LL);
+        b[e] = e ? b[e - 1] : scan_find(rows, B, r[e]);
+        while (r[e] >= rows[b[e] + 1]) ++b[e];     // ends: rows[B] = total > r
+        o[e] = a.len_old[b[e]];
       }
+#pragma unroll
+      for (int e = 0; e < PLAN_ROWS; ++e) {
+        const int p = o[e] + r[e] - rows[b[e]], j = p >> a.psh, have = (o[e] + T - 1) >> a.psh;
+        const gint from = (gint)(j < have ? (uintptr_t)(a.table + (size_t)b[e] * a.width + j)
+                                          : (uintptr_t)(a.free_pages + ring(taken[b[e]] + j - have)));
+        s[e] = *from;
+        o[e] = p & (T - 1);
+      }
+#pragma unroll
+      for (int e = 0; e < PLAN_ROWS; ++e)
+        s[e] = ((s[e] >= 0) & (s[e] < a.n_pages) & (r0 + e < total)) ? (s[e] << a.psh) + o[e] : -1;
     }
 #pragma unroll
     for (int e = 0; e < PLAN_ROWS; ++e)
