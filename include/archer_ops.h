@@ -166,8 +166,10 @@ archer_status archer_cache4_read(int32_t dtype, const archer_cache4 *cache, int3
  * fresh.  Q, K2, Vt2 and O 16-byte aligned.  workspace: device scratch of
  * archer_op_attention_cache4_ws_bytes bytes, 256-byte aligned (NULL if that is
  * 0); calls sharing a workspace must not overlap.  A row's result does not depend on
- * the other sequences' data, but on batch and max_cached, which choose the
- * split of the keys, to rounding. */
+ * the other sequences' data, but, to rounding, on batch, G, max_cached and the batch's
+ * lengths, which choose the kernel and the split of the keys.  fp16: probabilities are
+ * rounded to fp16, and where batch and G are large the queries to about 14 bits of the largest
+ * of 32 elements. */
 size_t archer_op_attention_cache4_ws_bytes(int32_t dtype, int32_t batch, int32_t G, int32_t Hq, int32_t Hkv,
                                            int32_t hd, int32_t max_cached, int32_t fresh);
 archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4 *cache, int32_t batch, int32_t G,

@@ -535,7 +535,7 @@ class Cache4:
     def __init__(self, data, page_size, head_dim):
         if data.dim() != 3:
             _refuse(E_SHAPE, "data must be [n_pages][n_kv_heads][page bytes]")
-        self.data = data
+        self._data = data
         self.n_pages, self.n_kv_heads, page_bytes = data.shape
         self.page_size, self.head_dim = page_size, head_dim
         self.desc = Cache4Desc(_dev(data, torch.uint8, "data", torch.cuda.current_device()), self.n_pages, page_size,
@@ -547,6 +547,11 @@ class Cache4:
         if n != data.numel():
             _refuse(E_SHAPE, f"a page of {page_size} tokens has {page_size * (head_dim + head_dim // 16)} bytes "
                              f"per head, not {page_bytes}")
+
+    @property
+    def data(self):
+        """The tensor that the descriptor points into: another one is another cache."""
+        return self._data
 
     @classmethod
     def empty(cls, n_pages, page_size, n_kv_heads, head_dim):

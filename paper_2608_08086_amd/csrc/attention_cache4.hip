@@ -174,7 +174,7 @@ __device__ __forceinline__ SeqView seq_view(const Attn4Args& a, int b) {
   v.len = min(max(a.cached_len[b], 0), cap);
   v.rows = a.resp_len ? min(max(a.resp_len[b], 0), a.G) : a.G;
   v.nfresh = a.K2 ? v.rows : 0;
-  v.steps1 = (v.len + a.step - 1) / a.step;
+  v.steps1 = (int)(((unsigned)v.len + a.step - 1) / a.step);
   v.steps = v.steps1 + (v.nfresh + a.step - 1) / a.step;
   return v;
 }
@@ -194,13 +194,25 @@ struct Work {
   int b, first, nsplit, chunk;   // b < 0: no such chunk
 };
 
+// Sequence `key` in the order of falling length, of the 64 that it is one of.
+__device__ __forceinline__ int by_length(const Attn4Args& a, int key) {
+  const int lane = threadIdx.x & 63, b0 = key & ~63, n = min(a.batch - b0, 64);
+  const int mine = seq_view(a, b0 + min(lane, n - 1)).steps;
+  int rank = lane < n ? 0 : 64;
+  for (int i = 0; i < n; ++i) {
+    const int other = __builtin_amdgcn_readlane(mine, i);
+    rank += (other > mine) | ((other == mine) & (i < lane));
+  }
+  return b0 + __ffsll(__ballot(rank == key - b0)) - 1;
+}
+
 // BY_SEQ: the chunks of sequence `key`; else the sequence of chunk `key`.
 template <bool BY_SEQ>
 __device__ __forceinline__ Work find_work(const Attn4Args& a, int key) {
   const int lane = threadIdx.x & 63;
   Work w{-1, 0, 1, INT_MAX};
   if (a.target == 0) {           // no splits: chunk b is sequence b
-    w.b = key < a.batch ? key : -1;
+    w.b = key;
     w.first = key;
     return w;
   }
@@ -610,19 +622,22 @@ __device__ __forceinline__ QTerms query_terms(const Frag<f16>* q, float mul) {
       top = max(top, __float_as_uint(x[8 * i + e]) & 0x7fffffffu);
     }
   }
-  // s1: the least power of two with max |q| <= 7.5 s1; 0 and tiny values take any
+  // s1 = 2^(e1 - 127): the least power of two with max |q| <= 7.5 s1; 0 and tiny values take any
   const unsigned e1 = max((top + 0x0fffffu) >> 23, 80u) - 2u;
-  // a residual of t1 is at most s1 / 4, of t2 s2 / 8: at most 4 of the next scale
-  const unsigned e[3] = {e1, e1 - 4u, e1 - 9u};
+  const float unit = __uint_as_float((254u - e1) << 23);
+  x *= unit;
+  // a residual of t1 is at most s1 / 4, of t2 s2 / 8: at most 4 of the next scale.  Through fp16
+  // only to choose the nearest e2m3, in units of s1, where fp16's own steps are far
+  // below the third term's; the residual is kept in fp32.
+  constexpr unsigned below[3] = {0, 4, 9};
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const float s = __uint_as_float(e[i] << 23);
-    // through fp16 only to choose the nearest e2m3: the residual is kept in fp32
+    const float s = __uint_as_float((127u - below[i]) << 23);
     r.t[i] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(__builtin_convertvector(x, f16x32), s);
     x -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.t[i], s);
   }
   // an infinite or NaN query element: NaN scores
-  r.scale = (top >= 0x7f800000u ? 255u : e[0]) | e[1] << 8 | e[2] << 16;
+  r.scale = (top >= 0x7f800000u ? 255u : e1) | (e1 - 4u) << 8 | (e1 - 9u) << 16;
   return r;
 }
 
@@ -662,7 +677,8 @@ __global__ __launch_bounds__(64 * RW, 2) void attn4_rows_kernel(Attn4Args a) {
   constexpr int HD = 128, CB = 2, KF = HD / 32, VF = HD / 16, NT = 64 * RW;
   using L = C4<HD>;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lg = lane >> 4, lc = lane & 15;
-  const int h = blockIdx.x % a.hkv, cg = blockIdx.x / a.hkv, b = blockIdx.y;
+  const int h = blockIdx.x % a.hkv, cg = blockIdx.x / a.hkv;
+  const int b = a.sorted ? __builtin_amdgcn_readfirstlane(by_length(a, blockIdx.y)) : (int)blockIdx.y;
   const int grp = a.hq / a.hkv, c0 = (cg * RW + w) * 16 * CB;
   // The queries and the first pages are requested before the lengths are waited for.
   const long qrows = (long)a.batch * a.G;
@@ -729,9 +745,9 @@ __global__ __launch_bounds__(64 * RW, 2) void attn4_rows_kernel(Attn4Args a) {
   unsigned alo, ahi;
   int avalid;
   auto place = [&](int page) __attribute__((always_inline)) {
-    const int k0 = (pbase + lane) * 32;
+    const unsigned k0 = (unsigned)(pbase + lane) * 32u;      // of the last tiles' lanes, up to 2^31 and some
     const bool ok = page >= 0 && page < a.c.n_pages;
-    avalid = ok ? min(max(v.len - k0, 0), 32) : 0;
+    avalid = ok ? min(max((int)((unsigned)v.len - k0), 0), 32) : 0;
     const uintptr_t p = (uintptr_t)(pool + (size_t)(ok ? page : 0) * page_stride + (size_t)((k0 & (Tp - 1)) * L::KROW));
     alo = (unsigned)p;
     ahi = (unsigned)(p >> 32);
@@ -1140,16 +1156,21 @@ Kind kind_of(int fp32, int batch, int G, int hq, int hkv, int hd) {
 }
 
 template <class T, int HD>
-void launch_kind(const Attn4Args& a, hipStream_t st) {
+void launch_kind(Attn4Args a, hipStream_t st) {
   const Kind kind = kind_of(sizeof(T) == 4, a.batch, a.G, a.hq, a.hkv, a.hd);
-  const long ncol = (long)a.G * (a.hq / a.hkv);
-  auto grid = [&](long cols) { return dim3((unsigned)(a.hkv * ((ncol + cols - 1) / cols)), (unsigned)a.slots); };
+  const long ncol = (long)a.G * (a.hq / a.hkv), cols = kind == Kind::COL1 ? 16 : kind == Kind::COL2 ? 32 : 256;
+  const dim3 grid((unsigned)(a.hkv * ((ncol + cols - 1) / cols)), (unsigned)a.slots);
+  // More workgroups than CUs: the longest sequences first, or the last ones to start are waited
+  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 143 us, not 151).  In the
+  // column kernel, several to a CU and shorter, it costs more than it gives (64 of 512 + 32
+  // keys, 32 rows, 32 heads: 65 us, not 54).
+  a.sorted = kind == Kind::WIDE && a.batch > 1 && (long)grid.x * a.batch > 256;
   if (kind == Kind::COL1) {
-    attn4_columns_kernel<T, HD, 1, NWAVE><<<grid(16), 64 * NWAVE, 0, st>>>(a);
+    attn4_columns_kernel<T, HD, 1, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
   } else if constexpr (sizeof(T) == 2) {
-    if (kind == Kind::COL2) attn4_columns_kernel<T, HD, 2, NWAVE><<<grid(32), 64 * NWAVE, 0, st>>>(a);
-    else if constexpr (HD == 128) attn4_rows_kernel<<<grid(256), 64 * RW, 0, st>>>(a);
-    else attn4_columns_kernel<T, HD, 4, 1><<<grid(256), 64 * NWAVE, 0, st>>>(a);
+    if (kind == Kind::COL2) attn4_columns_kernel<T, HD, 2, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
+    else if constexpr (HD == 128) attn4_rows_kernel<<<grid, 64 * RW, 0, st>>>(a);
+    else attn4_columns_kernel<T, HD, 4, 1><<<grid, 64 * NWAVE, 0, st>>>(a);
   }
   if (a.slots > a.batch) {
     constexpr int SL = 256 / (HD / 4);

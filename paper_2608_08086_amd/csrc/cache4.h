@@ -75,6 +75,7 @@ struct Attn4Args {
   float *Opart, *ML;            // chunk partials [slots][hkv][G * hq / hkv][hd], and (m, l) of each
   int batch, G, hq, hkv, hd;
   int target, chunk_min, slots, step; // see Attn4Split
+  int sorted;                   // row kernel: sequences in the order of falling length
   float scale_log2;
 };
 

@@ -171,7 +171,8 @@ def test_no_rows():
 class Case:
     """A batch over a cache whose unused bytes are anything (NaN scales among them)."""
 
-    def __init__(self, dtype, lens, G, hq, hkv, hd, page, fresh, resp=None, seed=0, q_scale=2.0, share=False):
+    def __init__(self, dtype, lens, G, hq, hkv, hd, page, fresh, resp=None, seed=0, q_scale=2.0, share=False,
+                 k_scale=1.0):
         rng = np.random.default_rng(seed)
         self.dtype, self.lens, self.G, self.hq, self.hkv, self.hd, self.page = dtype, lens, G, hq, hkv, hd, page
         B = len(lens)
@@ -191,8 +192,8 @@ class Case:
         self.K, self.V = [], []
         for b, n in enumerate(lens):
             slots = [self.table[b, p // page] * page + p % page for p in range(n)]
-            self.data = oc.write(self.data, page, hd, rng.standard_normal((hkv, n, hd)), rng.standard_normal((hkv, n, hd)),
-                                 slots)
+            self.data = oc.write(self.data, page, hd, rng.standard_normal((hkv, n, hd)) * k_scale,
+                                 rng.standard_normal((hkv, n, hd)), slots)
         for b, n in enumerate(lens):
             k, v = oc.read(self.data, page, hd, [self.table[b, p // page] * page + p % page for p in range(n)])
             self.K.append(k), self.V.append(v)
@@ -206,7 +207,7 @@ class Case:
             self.V2 = np.full((hkv, hd, self.ld2), np.nan, np_t)
             for b in range(B):
                 s = slice(b * self.stride, b * self.stride + rows[b])
-                self.K2[:, s] = rng.standard_normal((hkv, rows[b], hd))
+                self.K2[:, s] = rng.standard_normal((hkv, rows[b], hd)) * k_scale
                 self.V2[:, :, s] = rng.standard_normal((hkv, hd, rows[b]))
         self.rows = rows
 
@@ -373,6 +374,7 @@ SOME = np.r_[0, 1, 15:18, 31, 32, 63, 64, np.arange(97, 1024, 101), 127, 128, 25
     (list(range(41)), 100, 8, 8, 128, 256, True, None),
     ([2100, 40, 0, 1], 1024, 8, 8, 128, 128, True, [1024, 1000, 1024, 7]),       # more than 32 tiles
     ([0] * 8, 512, 8, 8, 128, 32, False, None),
+    ([(37 * b) % 150 for b in range(70)], 64, 8, 4, 128, 32, True, None),      # more sequences than a wave has lanes
     ([0, 31, 33, 70, 200, 1, 64, 9] * 2, 256, 16, 4, 64, 32, True, [256, 255, 0, 1, 17, 128, 200, 64] * 2),
     ([500, 20, 0, 300] * 4, 512, 8, 8, 64, 256, False, None),
 ])
@@ -389,6 +391,13 @@ WIDE_LENS = [300, 41, 0, 90, 64, 128, 7, 200]
 @pytest.mark.parametrize("hq,hkv,hd", WIDE)
 def test_wide_peaked_scores(hq, hkv, hd):
     c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 32, True, seed=31, q_scale=30.0)
+    c.check(c.run(), rows_of=SOME)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", WIDE)
+@pytest.mark.parametrize("q_scale,k_scale", [(2.0**-17, 2.0**12), (2.0**11, 2.0**-10)])
+def test_wide_small_and_large_queries(hq, hkv, hd, q_scale, k_scale):
+    c = Case(F16, WIDE_LENS, 512, hq, hkv, hd, 64, True, seed=35, q_scale=q_scale, k_scale=k_scale)
     c.check(c.run(), rows_of=SOME)
 
 
