@@ -444,6 +444,60 @@ def test_wide_same_bits_again_and_on_another_stream(hq, hkv, hd):
     assert torch.equal(a, b)
 
 
+# -- far pages, other lengths than the table's, several calls at once ------------------------------
+@pytest.mark.parametrize("G", [1, 20, 1040])
+def test_pages_beyond_4_gib(G):
+    """The same tokens in the first pages and in the last ones of a cache of 5 GB: the same bits."""
+    a = archer()
+    page, hkv, hd, n = 256, 8, 128, 700
+    n_pages = 5 * 10**9 // (hkv * page * (hd + hd // 16))
+    data = torch.empty(n_pages, hkv, page * (hd + hd // 16), dtype=torch.uint8, device="cuda")
+    data[:8] = 255
+    data[-8:] = 255
+    c = a.Cache4(data, page, hd)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    K, V = (torch.randn(hkv, n, hd, generator=g, device="cuda").half() for _ in range(2))
+    Q = torch.randn(hkv, 4 * G, hd, generator=g, device="cuda").half()
+    res = []
+    for pages in ([4, 1, 2], [n_pages - 1, n_pages - 6, n_pages - 3]):
+        t = torch.tensor(pages, device="cuda")
+        p = torch.arange(n, device="cuda")
+        slots = (t[p // page] * page + p % page).int()
+        a.cache4_write(c, K, V, slots)
+        k, v = a.cache4_read(c, slots)
+        assert torch.isfinite(k.float()).all() and torch.isfinite(v.float()).all()
+        table = t.int().repeat(4, 1).contiguous()
+        res.append((k, v, a.op_attention_cache4(Q, c, table, dev_i32([n, 1, 0, 511]), n)))
+    for x, y in zip(*res):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("G", [1, 80])
+def test_lengths_beyond_the_table_are_cut(G):
+    """A cached length (and max_cached) past the table's last page reads what the table has."""
+    c = Case(F16, [128, 96], G, 4, 2, 128, 32, True, seed=40)
+    c.table = c.table[:, :4].copy()
+    c.table[1, 3] = -1                             # sequence 1 has three pages
+    c.lens = [10**6, 2**31 - 1]
+    c.check(c.run(max_cached=2**31 - 1))
+
+
+def test_several_calls_at_once():
+    """Split attentions (each with its own workspace) and stores on three streams."""
+    cases = [Case(F16, [5000, 60], 1, 8, 2, 128, 64, False, seed=50 + i) for i in range(3)]
+    alone = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        out = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                out.append(c.run())
+        torch.cuda.synchronize()
+        for x, y in zip(alone, out):
+            assert torch.equal(x, y)
+
+
 # -- as they are used ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype,hq,hkv,hd,page", [(F16, 4, 2, 128, 32), (F32, 2, 2, 64, 64)])
 def test_plan_store_attend_rollback(dtype, hq, hkv, hd, page):
