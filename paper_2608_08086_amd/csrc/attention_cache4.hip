@@ -612,20 +612,22 @@ struct QTerms {
 __device__ __forceinline__ QTerms query_terms(const Frag<f16>* q, float mul) {
   QTerms r;
   f32x32 x;
-  unsigned top = 0;
+  // max |q| as an integer: infinities and NaN above the rest
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 t = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f16x8 v = q[i].v;
+  for (int i = 0; i < 4; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x8, q[i].v) & (unsigned short)0x7fff);
+  unsigned short th = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[8 * i + e] = (float)v[e] * mul;
-      top = max(top, __float_as_uint(x[8 * i + e]) & 0x7fffffffu);
-    }
-  }
+  for (int e = 0; e < 8; ++e) th = max(th, t[e]);
+  const unsigned top = __float_as_uint((float)__builtin_bit_cast(f16, th) * mul);
   // s1 = 2^(e1 - 127): the least power of two with max |q| <= 7.5 s1; 0 and tiny values take any
   const unsigned e1 = max((top + 0x0fffffu) >> 23, 80u) - 2u;
-  const float unit = __uint_as_float((254u - e1) << 23);
-  x *= unit;
+  const float unit = mul * __uint_as_float((254u - e1) << 23);      // q mul rounded to fp32, in units of s1
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[8 * i + e] = fmaf((float)q[i].v[e], unit, 0.f);
   // a residual of t1 is at most s1 / 4, of t2 s2 / 8: at most 4 of the next scale.  Through fp16
   // only to choose the nearest e2m3, in units of s1, where fp16's own steps are far
   // below the third term's; the residual is kept in fp32.
