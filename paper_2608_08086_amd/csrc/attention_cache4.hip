@@ -594,9 +594,9 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 //   * The probabilities' sum is a row of ones in P V.
 //   * The two waves of a SIMD are half a tile apart, with a barrier after each half: while
 //     one multiplies, the other one exponentiates and expands.
-// Measured, 32/32 heads, 256 rows: 8 sequences of 5376 keys 168 to 188 us (1.07 to 0.96 PF/s;
+// Measured, 32/32 heads, 256 rows: 8 sequences of 5376 keys 168 to 200 us (1.07 to 0.90 PF/s, as the clock allows;
 // a large fp16 library product reaches 1.22 on this GPU), 16 of 1344 cached and 256 fresh
-// keys 124 us (0.87 PF/s).  In cycles of a tile (about 3900 of both halves): P V 730, scores
+// keys 124 to 140 us (0.87 to 0.77 PF/s).  In cycles of a tile (about 3900 of both halves): P V 730, scores
 // 590, exponentials and loads 600 to 800, softmax 300, expansion 330, LDS stores 210 to
 // 340, and 600 of waiting at the barriers: the halves are not equally long.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
