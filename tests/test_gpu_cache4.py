@@ -589,6 +589,42 @@ def test_captured_turn_replays():
         assert res[4].item() == 0 and torch.isfinite(res[0].float()).all()
 
 
+def test_two_graphs_of_one_pool():
+    """Two captured attentions that share their memory pool, replayed in turn with other lengths, with eager calls
+    between: one whose sequences are cut (it needs a workspace), one of the row kernel."""
+    a = archer()
+    cases = [Case(F16, [5000, 60], 1, 8, 2, 128, 64, False, seed=60), Case(F16, WIDE_LENS, 512, 8, 4, 128, 64, True, seed=61)]
+    args, outs, graphs = [], [], []
+    for c in cases:
+        d = lambda x: None if x is None else dev(x, F16)  # noqa: E731
+        kw = dict(K2=d(c.K2), Vt2=d(c.V2), fresh_stride=c.stride)
+        args.append(((d(c.Q), new_cache(c.data, c.page, c.hd), dev_i32(c.table)), dev_i32(c.lens), max(c.lens), kw))
+        outs.append(torch.zeros(len(c.lens) * c.G, c.hq * c.hd, device="cuda", dtype=torch.bfloat16))
+
+    def call(i, O):
+        first, lens, most, kw = args[i]
+        a.op_attention_cache4(*first, lens, most, O=O, **kw)
+
+    for i in range(2):
+        call(i, outs[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, pool=graphs[0].pool() if graphs else None):
+            call(i, outs[i])
+        graphs.append(g)
+    for turn in range(3):
+        for c, x in zip(cases, args):
+            x[1].copy_(dev_i32([max(0, n - 7 * turn) for n in c.lens]))
+        for g in graphs:
+            g.replay()
+        got = [O.clone() for O in outs]
+        for i in range(2):
+            outs[i].zero_()
+            call(i, outs[i])
+            assert torch.equal(got[i], outs[i])
+
+
 # -- the binding's refusals ----------------------------------------------------------------------
 def test_binding_refusals():
     a = archer()
