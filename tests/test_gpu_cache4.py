@@ -291,6 +291,10 @@ def test_attention_matches_oracle(dtype, lens, G, hq, hkv, hd, page, fresh, resp
     (F32, [2500], 2, 4, 1, 64, 128, True),
     (F16, [4100], 100, 2, 2, 128, 64, True),
     (F16, [2047, 64, 0], 64, 2, 1, 64, 64, True),
+    # 1024 rows and more, few chunks
+    (F16, [3000], 32, 32, 16, 64, 32, False),
+    (F16, [3300], 32, 32, 8, 128, 64, True),
+    (F32, [4000], 32, 32, 32, 64, 32, True),
 ])
 def test_split_attention_matches_oracle(dtype, lens, G, hq, hkv, hd, page, fresh):
     say(f"split attention {dtype} lens={lens} G={G} hq={hq} hkv={hkv}")
@@ -300,6 +304,13 @@ def test_split_attention_matches_oracle(dtype, lens, G, hq, hkv, hd, page, fresh
     assert n > 0, "the case is meant to split"
     rows = None if G < 10 else np.arange(0, G, 7)
     say(f"  worst error / bound {c.check(c.run(), rows_of=rows):.3f}")
+
+
+def test_split_of_more_sequences_than_lanes():
+    """150 sequences of up to 1000 keys under a loose bound: chunks of 8 steps, found by a scan in three parts."""
+    c = Case(F16, [(137 * b) % 1001 for b in range(150)], 1, 2, 1, 64, 32, True, seed=4)
+    assert archer().lib.archer_op_attention_cache4_ws_bytes(0, 150, 1, 2, 1, 64, 10**6, 1) > 0
+    say(f"  worst error / bound {c.check(c.run(max_cached=10**6)):.3f}")
 
 
 @pytest.mark.parametrize("G", [1, 80])
