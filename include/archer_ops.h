@@ -168,8 +168,8 @@ archer_status archer_cache4_read(int32_t dtype, const archer_cache4 *cache, int3
  * 0); calls sharing a workspace must not overlap.  A row's result does not depend on
  * the other sequences' data, but, to rounding, on batch, G, max_cached and the batch's
  * lengths, which choose the kernel and the split of the keys.  fp16: probabilities are
- * rounded to fp16, and where batch and G are large the queries to about 14 bits of the largest
- * of 32 elements. */
+ * rounded to fp16, and where batch and G are large the queries to 2^-18 of the largest of
+ * 32 elements, which is less than the fp32 sums of the scores may be off by. */
 size_t archer_op_attention_cache4_ws_bytes(int32_t dtype, int32_t batch, int32_t G, int32_t Hq, int32_t Hkv,
                                            int32_t hd, int32_t max_cached, int32_t fresh);
 archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4 *cache, int32_t batch, int32_t G,

@@ -145,20 +145,38 @@ def attention(Q, K, V):
     return p @ V, p @ np.abs(V), float((top @ np.abs(K).T).max() / np.sqrt(hd)), float(np.abs(s).max())
 
 
-def attention_bound(O, A, qk, smax, n, hd, vmax, half):
+def score_sums(Q, K):
+    """Per query row, the largest sum |q k| / sqrt(hd) of its scores: as it is, and with each q taken as its 32
+    dimensions' largest."""
+    Q, K = np.abs(Q), np.abs(K)
+    top = np.repeat(Q.reshape(len(Q), -1, BLOCK).max(-1), BLOCK, axis=-1)
+    return tuple((x @ K.T).max(-1, keepdims=True) / np.sqrt(Q.shape[1]) for x in (Q, top))
+
+
+def attention_bound(O, A, qk, smax, n, hd, vmax, half, block=None):
     """Largest error of the library's kernels.  half: fp16 queries (fp16 probabilities, bf16 output) or fp32.
+    block None: qk is the second of `score_sums`, and any kernel may have run.  Else qk is the first, and block
+    the second where the row kernel runs (fp16, 128 dimensions, many rows) and 0 for the others.
 
     A score is a sum of hd products in fp32, each rounding at most 2^-24 of the running sum of magnitudes,
     then scaled and rounded: (hd + 3) 2^-24 qk, and 2^-23 smax for the exponent's argument.  The exponential
-    itself: 2^-22.  With fp16 queries the row kernel multiplies three e2m3 terms of each query element: the
+    itself: 2^-22.  With fp16 queries the row kernel multiplies four e2m3 terms of each query element: the
     first is off by at most 2^-2 of its scale s1 (half the largest step), the second, of scale s1 / 16 and at
-    most 4 of it, by 2^-3 s1 / 16, the third, of scale s1 / 512, by 2^-3 s1 / 512 = 2^-12 s1; s1 is the least power of two that
-    has the block's largest element below 7.5 s1, which therefore exceeds 3.75 s1: 2^-13.9 of it, 2^-13.9 qk in
-    a score.  These are relative errors of the probabilities, in the numerator and in the denominator.
+    most 4 of it, by 2^-3 s1 / 16, the third and the fourth, each of 2^-5 of the scale before and at most 4 of it, by
+    2^-3 s1 / 512 and 2^-3 s1 / 2^14 = 2^-17 s1; s1 is the least power of two that has the block's largest element
+    below 7.5 s1, which therefore exceeds 3.75 s1: 2^-18.9 of it, 2^-18.9 block in a score.  These are 4 hd
+    products: a term that overshoots is taken back by the next ones, by at most |q| where it is the element's first
+    (it is no more than twice |q|) and by at most s1 / 4 in all, so the terms' magnitudes add up to no more than 3.5 |q|
+    and |q| + 0.52 s1; and the sum starts from the reference, at most smax:
+    (4 hd + 4) 2^-24 (min(3.5 qk, qk + block / 7) + smax).
+    These are relative errors of the probabilities, in the numerator and in the denominator.
     Sums over n keys in fp32, with one rescale per 32 keys: (n + n / 16 + 40) 2^-24 in both.  fp16 probabilities:
     half a step is 2^-11 relative, and 2^-25 absolute where they are subnormal (the largest is between 1 and
     2^8, so that the denominator is at least 1).  The output's own rounding: bf16 2^-8, fp32 2^-24."""
-    rel = 2 * (((hd + 3) * 2.0**-24 + half * 2.0**-13.9) * qk + 2.0**-23 * smax + 2.0**-22 + (n + n / 16 + 40) * 2.0**-24)
+    rows = half if block is None else np.asarray(block) > 0
+    block = qk if block is None else block
+    rel = np.where(rows, (4 * hd + 4) * 2.0**-24 * (np.minimum(3.5 * qk, qk + block / 7) + smax) + 2.0**-18.9 * block, (hd + 3) * 2.0**-24 * qk)
+    rel = 2 * (rel + 2.0**-23 * smax + 2.0**-22 + (n + n / 16 + 40) * 2.0**-24)
     if not half:
         return 2.0**-24 * np.abs(O) + A * rel + 1e-30
     return 2.0**-8 * np.abs(O) + A * (rel + 2.0**-11) + n * 2.0**-25 * vmax + 1e-30

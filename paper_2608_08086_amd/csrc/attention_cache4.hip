@@ -5,7 +5,7 @@
 // fp16, so for fp16 queries the column kernel's only roundings are those of the fp16
 // attention beside it: the probabilities to fp16 and the output to bf16 (scores, running
 // maximum and sum and the accumulators are fp32).  The row kernel also writes a query as
-// three short terms; see there.
+// four short terms; see there.
 //
 // What bounds it: with few queries the cache's bytes, 17/16 D per key and head, at the
 // 5.3 TB/s that a read of a large array reaches; with many the matrix instructions of the
@@ -584,11 +584,14 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 // expanding a tile for every 32 columns is spent once for 256:
 //   * Scores on the codes themselves.  The fp4 x fp6 MFMA (16x16x128, block scales) takes
 //     a key's 32 codes of a lane and their scale byte as they are stored, at the
-//     rate of an fp16 16x16x32, so four times its work.  A query is the sum of three
+//     rate of an fp16 16x16x32, so four times its work.  A query is the sum of four
 //     e2m3 terms per 32 dimensions, each term's scale a power of two:
-//       q = t1 + t2 + t3 + r,  |r| <= 2^-12 s1,  s1 = the scale of t1, max |q| > 3.75 s1,
-//     an error of at most 2^-13.9 of the largest element of the 32.  Three
-//     MFMAs do what four fp16 ones would, and no key is expanded.  The queries
+//       q = t1 + t2 + t3 + t4 + r,  |r| <= 2^-17 s1,  s1 = the scale of t1, max |q| > 3.75 s1,
+//     an error of at most 2^-18.9 of the largest element of the 32, less than the fp32 sums may be
+//     off by.  Four MFMAs do what four fp16 ones would, and no key is expanded.  (Three terms:
+//     2^-13.9, which is more than the fp16 probabilities' rounding where scores are large or one of the 32
+//     elements outweighs the others; 39.2 us in place of 40.7 for 8 sequences of 512 + 256 keys, 174 in
+//     place of 190 for 8 of 5376.)  The queries
 //     carry the softmax's factor, and the MFMA starts from minus the column's reference,
 //     so that a score comes out as the exponent of its probability.
 //   * Values are expanded by all eight waves, one tile ahead, into the operand
@@ -596,19 +599,19 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 //   * The probabilities' sum is a row of ones in P V.
 //   * The two waves of a SIMD are half a tile apart, with a barrier after each half: while
 //     one multiplies, the other one exponentiates and expands.
-// Measured, 32/32 heads, 256 rows: 8 sequences of 5376 keys 168 to 200 us (1.07 to 0.90 PF/s, as the clock allows;
-// a large fp16 library product reaches 1.22 on this GPU), 16 of 1344 cached and 256 fresh
-// keys 124 to 140 us (0.87 to 0.77 PF/s).  In cycles of a tile (about 3900 of both halves): P V 730, scores
+// Measured, 32/32 heads, 256 rows, back to back: 8 sequences of 5376 keys 190 us (0.95 PF/s; a large fp16
+// library product reaches 1.22 on this GPU), 16 of 1344 cached and 256 fresh keys 155 us (0.69 PF/s).
+// The halves are not equally long: with three terms, in cycles of a tile (about 3900 of both), P V 730, scores
 // 590, exponentials and loads 600 to 800, softmax 300, expansion 330, LDS stores 210 to
-// 340, and 600 of waiting at the barriers: the halves are not equally long.
+// 340, and 600 of waiting at the barriers.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 typedef _Float16 f16x32 __attribute__((ext_vector_type(32)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
-// Three e2m3 terms of a lane's 32 query elements times `mul`, and their scale bytes.
+// Four e2m3 terms of a lane's 32 query elements times `mul`, and their scale bytes.
 struct QTerms {
-  u32x6 t[3];
+  u32x6 t[4];
   unsigned scale;    // byte i: the biased exponent of term i
 };
 __device__ __forceinline__ QTerms query_terms(const Frag<f16>* q, float mul) {
@@ -630,18 +633,18 @@ __device__ __forceinline__ QTerms query_terms(const Frag<f16>* q, float mul) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[8 * i + e] = fmaf((float)q[i].v[e], unit, 0.f);
-  // a residual of t1 is at most s1 / 4, of t2 s2 / 8: at most 4 of the next scale.  Through fp16
-  // only to choose the nearest e2m3, in units of s1, where fp16's own steps are far
-  // below the third term's; the residual is kept in fp32.
-  constexpr unsigned below[3] = {0, 4, 9};
+  // a residual of t1 is at most s1 / 4, of the others an eighth of their scale: at most 4 of the next
+  // scale.  Through fp16 only to choose the nearest e2m3, in units of s1, where fp16's own steps
+  // (2^-24 at least) are far below the fourth term's 2^-17; the residual is kept in fp32.
+  constexpr unsigned below[4] = {0, 4, 9, 14};
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const float s = __uint_as_float((127u - below[i]) << 23);
     r.t[i] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(__builtin_convertvector(x, f16x32), s);
     x -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.t[i], s);
   }
   // an infinite or NaN query element: NaN scores
-  r.scale = (top >= 0x7f800000u ? 255u : e1) | (e1 - 4u) << 8 | (e1 - 9u) << 16;
+  r.scale = (top >= 0x7f800000u ? 255u : e1) | (e1 - 4u) << 8 | (e1 - 9u) << 16 | (e1 - 14u) << 24;
   return r;
 }
 
@@ -1017,14 +1020,15 @@ __global__ __launch_bounds__(64 * RW, 2) void attn4_rows_kernel(Attn4Args a) {
         constexpr int I = x.value;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          sc[cb][0] = mfma_codes<0, I>(k[0], ks, q[cb], I == 2 ? ref[cb] : sc[cb][0]);
-          sc[cb][1] = mfma_codes<1, I>(k[1], ks, q[cb], I == 2 ? ref[cb] : sc[cb][1]);
-          sc[cb][2] = mfma_codes<2, I>(k[2], ks, q[cb], I == 2 ? ref[cb] : sc[cb][2]);
-          sc[cb][3] = mfma_codes<3, I>(k[3], ks, q[cb], I == 2 ? ref[cb] : sc[cb][3]);
+          sc[cb][0] = mfma_codes<0, I>(k[0], ks, q[cb], I == 3 ? ref[cb] : sc[cb][0]);
+          sc[cb][1] = mfma_codes<1, I>(k[1], ks, q[cb], I == 3 ? ref[cb] : sc[cb][1]);
+          sc[cb][2] = mfma_codes<2, I>(k[2], ks, q[cb], I == 3 ? ref[cb] : sc[cb][2]);
+          sc[cb][3] = mfma_codes<3, I>(k[3], ks, q[cb], I == 3 ? ref[cb] : sc[cb][3]);
         }
         __builtin_amdgcn_sched_barrier(0);
       };
       __builtin_amdgcn_sched_barrier(0);
+      term(std::integral_constant<int, 3>());
       term(std::integral_constant<int, 2>());
       term(std::integral_constant<int, 1>());
       term(std::integral_constant<int, 0>());
