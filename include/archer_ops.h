@@ -152,7 +152,7 @@ archer_status archer_cache4_read(int32_t dtype, const archer_cache4 *cache, int3
  * sequence's fresh keys; no other mask, scale 1 / sqrt(hd).  Types and heads
  * as archer_op_attention (hd and Hkv are the cache's).
  *   Q          [Hq][batch G][hd]: G query rows per sequence
- *   O          [batch G][Hq hd]: a row without any key gives zeros
+ *   O          [batch G][Hq hd]: a row without any key gives zeros, one whose scores are all -infinity NaN
  *   table      device int32 [batch][max_pages]; the keys of an entry outside
  *              [0, n_pages) are left out
  *   cached_len device int32 [batch], >= 0; no more than max_cached (host; sizes the

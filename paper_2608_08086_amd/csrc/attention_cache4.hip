@@ -145,6 +145,14 @@ __device__ __forceinline__ int key_row(int kb, int r) { return 8 * (r >> 2) + 4 
 template <class T> struct OutOf { using type = bf16; };
 template <> struct OutOf<float> { using type = float; };
 
+// Running maximum before the first key: below every score, and finite, so that
+// no difference of maxima is a NaN; and after keys whose scores are all -infinity
+// (an infinite query or key element), so that a row of these is told from one without keys.
+constexpr float M_NONE = -3.0e38f, M_KEYS = -2.9e38f;
+
+// The softmax's sum, of running maximum m: without keys 0, with none but -infinite scores NaN.
+__device__ __forceinline__ float final_sum(float l, float m) { return l == 0.f && m > M_NONE ? NAN : l; }
+
 // four dimensions of an output row: x / l, or zeros where there was no key
 template <class OT>
 __device__ __forceinline__ void store_row4(OT* p, f32x4 x, float l) {
@@ -254,10 +262,6 @@ template <int HD> struct Raw {
   unsigned v[C4<HD>::VUNIT / 4];
   u32x2 ks, vs;                // scales of 8 keys each
 };
-
-// Running maximum before the first key: below every score, and finite, so that
-// no difference of maxima is a NaN.
-constexpr float M_NONE = -3.0e38f;
 
 // A column's reference is raised, and its accumulators rescaled, when a score
 // exceeds it by more than this (log2): probabilities are then at most 2^RESCALE, whose fp16
@@ -420,9 +424,11 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
     load_values(ts, max(page, 0));
   }
   int n = 0;                                  // steps of `pages` already requested
+  bool keys = false;                          // the wave had a key
   for (int t = ts; t < te; t += KW) {
     // a page that the cache does not have: none of its keys count
     const int valid = page < 0 ? 0 : v.len - t * STEP;
+    keys |= valid > 0;
     if (++n == 64) {
       pages = pages_from(t + KW);
       asm volatile("" : "+v"(pages));         // waits for them here, not in every step
@@ -469,6 +475,7 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
   if (t < v.steps1) t += (v.steps1 - t + KW - 1) / KW * KW;
   for (; t < t1; t += KW) {
     const int k0 = (t - v.steps1) * STEP, f0 = b * a.fstride + k0, valid = v.nfresh - k0;
+    keys = true;
     // every fragment of the keys, then of the values, is requested before the
     // first is used; keys past the end read the last one's, masked below
     Frag<T> k[KF][2];
@@ -504,7 +511,10 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
   };
   auto part_row = [&](int col) __attribute__((always_inline)) { return ((size_t)slot * a.hkv + h) * ((size_t)a.G * grp) + col; };
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) l_run[cb] = sum_groups(l_run[cb]);
+  for (int cb = 0; cb < CB; ++cb) {
+    l_run[cb] = sum_groups(l_run[cb]);
+    m_run[cb] = fmaxf(m_run[cb], keys ? M_KEYS : M_NONE);
+  }
   if constexpr (KW == 1) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -517,7 +527,7 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 #pragma unroll
         for (int j = 0; j < VF; j += 4) {
           const f32x4 x = {o[cb][j][e], o[cb][j + 1][e], o[cb][j + 2][e], o[cb][j + 3][e]};
-          if (wk.nsplit == 1) store_row4<OT>(out + (4 * lg + e) * VF + j, x, l_run[cb]);
+          if (wk.nsplit == 1) store_row4<OT>(out + (4 * lg + e) * VF + j, x, final_sum(l_run[cb], m_run[cb]));
           else *(f32x4*)(a.Opart + at * HD + (4 * lg + e) * VF + j) = x;
         }
       if (wk.nsplit > 1 && lg == 0) *(float2*)(a.ML + at * 2) = make_float2(m_run[cb], l_run[cb]);
@@ -566,7 +576,7 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
             x += *(const f32x4*)&so[k][c][d];
           }
           if (wk.nsplit == 1) {
-            store_row4<OT>(out_row(col) + half * HH + d, x, l);
+            store_row4<OT>(out_row(col) + half * HH + d, x, final_sum(l, smax[cb * 16 + c]));
           } else {
             const size_t at = part_row(col);
             *(f32x4*)(a.Opart + at * HD + half * HH + d) = x;
@@ -836,7 +846,9 @@ __global__ __launch_bounds__(64 * RW, 2) void attn4_rows_kernel(Attn4Args a) {
   // probabilities: masks the scores, and sees that none exceeds its column's
   // reference by too much
   Frag<f16> pf[CB][2];
+  int keys = 0;         // not 0: a tile had a key
   auto softmax = [&](int val) __attribute__((always_inline)) {
+    keys |= val;
     if (val != (32 | 32 << 16)) {
       const int k0 = 8 * local_value(lg), n0 = (val & 0xffff) - k0, n1 = (val >> 16) - k0;
 #pragma unroll
@@ -1046,7 +1058,7 @@ __global__ __launch_bounds__(64 * RW, 2) void attn4_rows_kernel(Attn4Args a) {
   char* buf = lds + w * OUT;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    const float inv = l[cb][0] == 0.f ? 0.f : 1.0f / l[cb][0];
+    const float sum = final_sum(l[cb][0], keys ? M_KEYS : M_NONE), inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -1125,6 +1137,7 @@ __global__ __launch_bounds__(256) void attn4_merge_kernel(Attn4Args a) {
     float M = M_NONE;
 #pragma unroll
     for (int s = 0; s < SL; ++s) M = fmaxf(M, sm[s]);
+    m = M;
     l = 0.f;
     x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -1134,7 +1147,7 @@ __global__ __launch_bounds__(256) void attn4_merge_kernel(Attn4Args a) {
       x += sx[s][d / 4] * f;
     }
   }
-  store_row4<OT>((OT*)a.O + ((size_t)b * a.G + col / grp) * ((size_t)a.hq * HD) + (size_t)(h * grp + col % grp) * HD + d, x, l);
+  store_row4<OT>((OT*)a.O + ((size_t)b * a.G + col / grp) * ((size_t)a.hq * HD) + (size_t)(h * grp + col % grp) * HD + d, x, final_sum(l, m));
 }
 
 // Which kernel a call takes, by its number of columns (us on a GPU of 256 CUs, cached +
