@@ -525,8 +525,10 @@ def _i32(t, n, name, dev):
     return _dev(t, torch.int32, name, dev)
 
 
-# the current stream of a device as an address (a torch.cuda.Stream object takes 3 us to make)
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# The current stream of a device as an address.  A torch.cuda.Stream object takes 3 us to make; the
+# call that makes none is not public, and a torch without it takes the longer way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 class Cache4:
