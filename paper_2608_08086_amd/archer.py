@@ -525,6 +525,13 @@ def _i32(t, n, name, dev):
     return _dev(t, torch.int32, name, dev)
 
 
+def _int(x, name):
+    """A host integer of the C ABI: ctypes would pass one beyond 32 bits as its low 32."""
+    if not -2**31 <= x < 2**31:
+        _refuse(E_SHAPE, f"{name} must fit in 32 bits")
+    return x
+
+
 # The current stream of a device as an address.  A torch.cuda.Stream object takes 3 us to make; the
 # call that makes none is not public, and a torch without it takes the longer way.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -538,8 +545,8 @@ class Cache4:
         if data.dim() != 3:
             _refuse(E_SHAPE, "data must be [n_pages][n_kv_heads][page bytes]")
         self._data = data
-        self.n_pages, self.n_kv_heads, page_bytes = data.shape
-        self.page_size, self.head_dim = page_size, head_dim
+        self.n_pages, self.n_kv_heads, page_bytes = (_int(n, "a dimension of data") for n in data.shape)
+        self.page_size, self.head_dim = _int(page_size, "page_size"), _int(head_dim, "head_dim")
         self.desc = Cache4Desc(_dev(data, torch.uint8, "data", torch.cuda.current_device()), self.n_pages, page_size,
                                self.n_kv_heads, head_dim)
         self.ref = C.byref(self.desc)
@@ -569,11 +576,11 @@ def cache4_plan(len_old, len_new, page_size, table, free_pages, pool, slot_rows)
         _refuse(E_SHAPE, "table must be [batch][max_pages]")
     n_pages, width = free_pages.numel(), table.shape[1]
     ptrs = (_i32(len_old, B, "len_old", dev), _i32(len_new, B, "len_new", dev))
-    rows = max(slot_rows, 0)
+    rows = max(_int(slot_rows, "slot_rows"), 0)
     out = torch.empty(rows + B + 4, dtype=torch.int32, device=len_old.device)
     p = out.data_ptr()
     slot_map, row_off, pool_out, status = out.split((rows, B + 1, 2, 1))
-    _check(lib.archer_cache4_plan(B, *ptrs, page_size, n_pages, width, _i32(table, B * width, "table", dev),
+    _check(lib.archer_cache4_plan(B, *ptrs, _int(page_size, "page_size"), n_pages, width, _i32(table, B * width, "table", dev),
                                   _i32(free_pages, n_pages, "free_pages", dev), _i32(pool, 2, "pool", dev),
                                   p + 4 * (rows + B + 1), p + 4 * rows, p, slot_rows, p + 4 * (rows + B + 3),
                                   _raw_stream(dev)))
@@ -628,6 +635,7 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
     if B < 1 or rows % B or hd != cache.head_dim:
         _refuse(E_SHAPE, "Q must hold G rows of head_dim for every row of the table")
     G, Hkv = rows // B, cache.n_kv_heads
+    _int(max_cached, "max_cached"), _int(fresh_stride, "fresh_stride")
     k2 = v2 = None
     ld2 = 0
     if K2 is not None or Vt2 is not None:
