@@ -131,7 +131,8 @@ archer_status archer_cache4_plan(int32_t batch, const int32_t *len_old, const in
  * unspecified mixture is stored); rows >= 0.  Element (head, row, d) is at
  * K[head k_head + row k_row + d] and V[head v_head + row v_row + d v_dim] (strides in
  * elements, any sign), with v_dim = 1 or v_row = 1: the prompt cache's
- * transposed values are stored as they lie (else ARCHER_E_UNSUPPORTED).
+ * transposed values are stored as they lie (else ARCHER_E_UNSUPPORTED; of a single row
+ * any v_dim will do).
  * Per 32 dimensions the scale is 2^e, e the least integer with max |x| <= 7 * 2^e,
  * clamped to [-23, 13]; elements are rounded to the nearest e2m1 value of
  * x / 2^e, ties to the even code, and saturate at 6 * 2^e (49152 at most).  Every

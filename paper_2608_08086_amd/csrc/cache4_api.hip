@@ -100,6 +100,7 @@ archer_status archer_cache4_write(int32_t dtype, const archer_cache4* cache, int
   if (!K || !V || !slot_map) return archer_fail(ARCHER_E_ARG, "null operand");
   const uintptr_t esz = dtype == ARCHER_BF16 ? 2 : 4;
   if (((uintptr_t)K | (uintptr_t)V) & (esz - 1)) return archer_fail(ARCHER_E_ARG, "K and V must be aligned to their elements");
+  if (rows == 1) v_row = 1;      // nothing is a row apart: a view's row stride then says nothing
   if (v_dim != 1 && v_row != 1)
     return archer_fail(ARCHER_E_UNSUPPORTED, "V must have unit stride along its dimensions or along its rows");
   C4RowsArgs a;
