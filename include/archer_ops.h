@@ -1,11 +1,13 @@
 /*
  * archer_ops.h -- single-kernel entry points and timing of the Archer library.
  *
- * These calls run one kernel of the decoding path exactly as the model path
- * launches it (same kernels, same tile and split choices for the same
- * shapes), on caller-provided device buffers.  They exist so that the
+ * archer_op_gemm, archer_op_attention and archer_op_attention_noalloc run one kernel of the
+ * decoding path exactly as the model path launches it (same kernels, same tile and split
+ * choices for the same shapes), on caller-provided device buffers.  They exist so that the
  * kernels can be checked element by element at full model sizes and timed in
- * isolation.  Conventions as in archer.h: device pointers, caller-owned
+ * isolation.  The 4-bit paged prompt cache's calls are operators of their own, for
+ * programs that hold prompts in it: the decoding path keeps its fp16 cache and
+ * runs none of them.  Conventions as in archer.h: device pointers, caller-owned
  * memory, asynchronous on the given stream, host-side argument checks.
  */
 #ifndef ARCHER_OPS_H
@@ -85,7 +87,8 @@ archer_status archer_op_attention_noalloc(int32_t dtype, int32_t Mq, int32_t Hq,
  * dimensions: 136 instead of 512 bytes per token and head of 128 dimensions.
  * Tokens live in pages of page_size tokens; a slot is
  * page * page_size + position in the page, and a sequence's row of a block
- * table lists its pages in order.  Several sequences may list the same page.
+ * table lists its pages in order.  The table of a read or an attention may list a
+ * page in several rows; a plan's may not (archer_cache4_plan).
  *
  * data: device, 16-byte aligned, archer_cache4_bytes bytes, caller-owned.
  * [n_pages][n_kv_heads] blocks of page_size * (head_dim + head_dim / 16) bytes:
@@ -116,6 +119,11 @@ size_t archer_cache4_bytes(const archer_cache4 *cache);
  *   status      [1]: 0, or why nothing was changed (pool_out = pool_in, row_off 0,
  *               slot_map -1): 1 too few free pages, 2 a length is negative or beyond
  *               max_pages, 3 more than slot_rows rows, 4 the pool is inconsistent
+ * A plan counts no references: every page that it is to take, keep or give back must be the
+ * page of one request, once, and not be free.  A page shared by several sequences
+ * belongs to one of them here; the others list it in tables of their own, and its owner
+ * must not shrink below it while they do (it would be handed out again).  This
+ * is not checked.
  * Pages are taken from the ring's front in request order and given back behind
  * its end, those of this call for later ones.  Called again with the same
  * arguments it gives the same results.  The arrays must not overlap. */
