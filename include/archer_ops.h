@@ -165,7 +165,8 @@ archer_status archer_cache4_read(int32_t dtype, const archer_cache4 *cache, int3
  *   table      device int32 [batch][max_pages]; the keys of an entry outside
  *              [0, n_pages) are left out
  *   cached_len device int32 [batch], >= 0; no more than max_cached (host; sizes the
- *              launch) and max_pages * page_size keys are read
+ *              launch: of more than 32768 it has every sequence's keys looked at for a split,
+ *              which short ones pay for) and max_pages * page_size keys are read
  *   K2, Vt2    [Hkv][ld2][hd], [Hkv][hd][ld2], or both NULL: sequence b's fresh keys
  *              are rows b fresh_stride .. + resp_len[b] - 1; ld2 and fresh_stride multiples of
  *              8, fresh_stride >= G, batch fresh_stride <= ld2

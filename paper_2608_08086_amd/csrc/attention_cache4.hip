@@ -1212,6 +1212,19 @@ void launch_kind(Attn4Args a, hipStream_t st) {
 //   B  4,  4096,       1,     32/8          20.9   14.7
 //   B 32,  2500,       1,     32/8          18.4   22.8
 //   B  8,  2000 + 8,   8,     28/4          16.8   20.6
+// That is for sequences of one length, which is all that the host knows.  Where one of them may be
+// far longer, its workgroup alone may walk for long, so a call of more than 1024 steps (130 us)
+// is cut whatever the batch would take together; the chunks are made of the lengths there are, about
+// one to a sequence where these are alike.  Up to 256 sequences: every wave scans their lengths.
+//                                           unsplit   split
+//   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     737    37
+//   B 40, one of 131072, 39 of 1000,      1,     28/4           550    27
+//   B 200, one of 40000, 199 of 1000,     1,     32/8           244    76
+//   B 20, 33000 each,                     1,     32/8           211   147
+//   B 64, 33000 each,                     1,     32/8           379   388
+//   B 64, 33000 each,                     8,     28/4           401   415
+//   B 64, 1000 each, max_cached 131072,   1,     32/8            12    18   (what a loose bound costs)
+//   B 200, 1000 each, max_cached 131072,  1,     32/8            28    52
 Attn4Split attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh) {
   const Kind kind = kind_of(fp32, batch, G, hq, hkv, hd);
   if (kind == Kind::WIDE) return Attn4Split{0, 0, batch, hd == 128 ? TILE : STEP};
@@ -1220,11 +1233,13 @@ Attn4Split attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int 
   Attn4Split s{0, 2 * NWAVE, batch, STEP};
   // One round of what the CUs hold (four workgroups of one block each, two of the others): cutting
   // B sequences by one length leaves up to B chunks more than that length divides out.
-  const long target = 256 * (kind == Kind::COL1 && !fp32 ? 4 : 2) / groups - batch;
+  long target = 256 * (kind == Kind::COL1 && !fp32 ? 4 : 2) / groups - batch;
+  const bool far = steps > 1024 && batch <= 256;
+  if (far) target = std::max(target, (long)batch);
   // (the kernels count a batch's steps in 32 bits)
-  if (target <= batch || steps * batch > INT_MAX) return s;
+  if ((target <= batch && !far) || steps * batch > INT_MAX) return s;
   const long chunk = std::max((steps * batch + target - 1) / target, (long)s.chunk_min);
-  if (steps - std::max(chunk, steps * batch * groups / 160) > 56) {
+  if (far || steps - std::max(chunk, steps * batch * groups / 160) > 56) {
     s.target = (int)target;
     s.slots = (int)std::min(target + batch, batch * ((steps + s.chunk_min - 1) / s.chunk_min));
   }
