@@ -179,7 +179,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache4_plan_kernel(C4PlanArgs a)
 }
 
 void launch_cache4_plan(const C4PlanArgs& a, hipStream_t st) {
-  const long items = std::max<long>((long)(a.slot_rows + PLAN_ROWS - 1) / PLAN_ROWS, a.batch);
+  const long items = std::max<long>(((long)a.slot_rows + PLAN_ROWS - 1) / PLAN_ROWS, a.batch);
   const unsigned grid = (unsigned)std::min<long>(std::max<long>((items + PLAN_THREADS - 1) / PLAN_THREADS, 1), 512);
   cache4_plan_kernel<<<grid, PLAN_THREADS, 3 * (a.batch + 1) * sizeof(int), st>>>(a);
 }
