@@ -609,11 +609,12 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 //   * The probabilities' sum is a row of ones in P V.
 //   * The two waves of a SIMD are half a tile apart, with a barrier after each half: while
 //     one multiplies, the other one exponentiates and expands.
-// Measured, 32/32 heads, 256 rows, back to back: 8 sequences of 5376 keys 190 us (0.95 PF/s; a large fp16
-// library product reaches 1.22 on this GPU), 16 of 1344 cached and 256 fresh keys 155 us (0.69 PF/s).
-// The halves are not equally long: with three terms, in cycles of a tile (about 3900 of both), P V 730, scores
-// 590, exponentials and loads 600 to 800, softmax 300, expansion 330, LDS stores 210 to
-// 340, and 600 of waiting at the barriers.
+// Measured, 32/32 heads, 256 rows, back to back (the clock falls by a tenth in the longer ones): 8 sequences of
+// 5376 keys 190 to 200 us (0.95 to 0.90 PF/s; a large fp16 library product reaches 1.22 on this GPU),
+// 8 of 512 cached and 256 fresh keys 40 us, 16 of 1344 and 256 132 to 159.  Of the cycles the
+// matrix pipes are busy in 56 %, a wave waits in 21 %.  A tile takes about 3900 in both halves: P V 730,
+// scores 790, exponentials and loads 600 to 800, softmax 300, expansion 330, LDS stores 210 to
+// 340, and the rest waiting at the barriers, for the halves are not equally long.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 typedef _Float16 f16x32 __attribute__((ext_vector_type(32)));
@@ -1157,14 +1158,14 @@ __global__ __launch_bounds__(256) void attn4_merge_kernel(Attn4Args a) {
 //     (64), two waves fit a SIMD: B 32, 2000 + 8 keys, 8 rows, 28/4 heads: 18.5, four 28.4.
 //   WIDE: columns enough that a workgroup's 256 (head_dim 128, row kernel) or 4 x 64
 //     (head_dim 64, four blocks a wave) occupy half of the CUs, or all of them twice:
-//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   130   COL2 197
-//       B  8, 512 + 256,       256,      32/32          39         59
-//       B 16, 1000 + 128,      128,      16/16          35         37
-//       B  4, 512 + 256,       256,      32/32          35         35
-//       B  2, 4096,            256,      32/32          51 + 10    47    (so not here)
-//       B  8, 1024 + 70,        70,      32/32          33         29    (nor here)
-//       B 16, 1344 + 256,      256,      32/32, 64 dim. 90        105
-//       B  8, 512 + 256,       256,      16/16, 64 dim. 26         19    (nor here)
+//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   153   COL2 208
+//       B  8, 512 + 256,       256,      32/32          41         64
+//       B 16, 1000 + 128,      128,      16/16          35         39
+//       B  4, 512 + 256,       256,      32/32          34         34
+//       B  2, 4096 + 256,      256,      32/32         117         54    (so not here)
+//       B  8, 1024 + 70,        70,      32/32          32         29    (nor here)
+//       B 16, 1344 + 256,      256,      32/32, 64 dim. 83         98
+//       B  8, 512 + 256,       256,      16/16, 64 dim. 27         19    (nor here)
 enum class Kind { COL1, COL2, WIDE };
 Kind kind_of(int fp32, int batch, int G, int hq, int hkv, int hd) {
   const long ncol = (long)G * (hq / hkv), all = ncol * batch * hkv;
@@ -1182,7 +1183,7 @@ void launch_kind(Attn4Args a, hipStream_t st) {
   const long ncol = (long)a.G * (a.hq / a.hkv), cols = kind == Kind::COL1 ? 16 : kind == Kind::COL2 ? 32 : 256;
   const dim3 grid((unsigned)(a.hkv * ((ncol + cols - 1) / cols)), (unsigned)a.slots);
   // More workgroups than CUs: the longest sequences first, or the last ones to start are waited
-  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 143 us, not 151).  In the
+  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 155 us, not 166).  In the
   // column kernel, several to a CU and shorter, it costs more than it gives (64 of 512 + 32
   // keys, 32 rows, 32 heads: 65 us, not 54).
   a.sorted = kind == Kind::WIDE && a.batch > 1 && (long)grid.x * a.batch > 256;
@@ -1205,8 +1206,8 @@ void launch_kind(Attn4Args a, hipStream_t st) {
 
 // A workgroup of four waves takes about 0.13 us for a step of its sequence, and about 160 of
 // them together what the memory (one block) or the CUs (two) can do.  Cutting the sequences
-// costs the merge's launch and a second pass over the queries, 4 to 8 us, so it has to
-// save more than 56 steps.  Unsplit and split:
+// costs the merge's launch and a second pass over the queries, 4 to 8 us (part of it the merge's own
+// scan of the lengths), so it has to save more than 56 steps.  Unsplit and split:
 //   B  1,  2500 keys,  1 row, 32/8 heads    13.9   15.0
 //   B  4,  2500,       1,     32/8          14.7   13.7
 //   B  4,  4096,       1,     32/8          20.9   14.7

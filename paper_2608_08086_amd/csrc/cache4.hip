@@ -20,7 +20,8 @@
 // thousand numbers from L2) rather than wait for one that does, and
 // takes the slots from the sums, not from the table that others are writing.
 // Bound by the chain of dependent loads (lengths, then a length and a page per slot) and
-// the launch: 4.6 us for 64 requests that grow by one token, 9.8 us for 1024 of which a
+// the launch, and with many slots by the rounds of that chain and its search over the grid's
+// threads: 4.6 us for 64 requests that grow by one token, 9.8 us for 1024 of which a
 // quarter gives its pages back and the others grow by up to 2048 (3 MB of slots).
 constexpr int PLAN_THREADS = 256;
 constexpr int PLAN_ROWS = 4;     // slots a thread makes with one search
