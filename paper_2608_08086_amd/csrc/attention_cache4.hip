@@ -1216,7 +1216,9 @@ void launch_kind(Attn4Args a, hipStream_t st) {
 // That is for sequences of one length, which is all that the host knows.  Where one of them may be
 // far longer, its workgroup alone may walk for long, so a call of more than 1024 steps (130 us)
 // is cut whatever the batch would take together; the chunks are made of the lengths there are, about
-// one to a sequence where these are alike.  Up to 256 sequences: every wave scans their lengths.
+// one to a sequence where these are alike.  Up to 256 sequences: every wave scans their lengths.  Not where the
+// key heads and blocks of one sequence are a round of workgroups by themselves (the partial results
+// are twice its queries): there is nothing to gain (fp32, 128 rows, 32/32 heads, half a round: 1048, 1025).
 //                                           unsplit   split
 //   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     737    37
 //   B 40, one of 131072, 39 of 1000,      1,     28/4           550    27
@@ -1234,8 +1236,9 @@ Attn4Split attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int 
   Attn4Split s{0, 2 * NWAVE, batch, STEP};
   // One round of what the CUs hold (four workgroups of one block each, two of the others): cutting
   // B sequences by one length leaves up to B chunks more than that length divides out.
-  long target = 256 * (kind == Kind::COL1 && !fp32 ? 4 : 2) / groups - batch;
-  const bool far = steps > 1024 && batch <= 256;
+  const long round = 256 * (kind == Kind::COL1 && !fp32 ? 4 : 2);
+  long target = round / groups - batch;
+  const bool far = steps > 1024 && batch <= 256 && groups < round;
   if (far) target = std::max(target, (long)batch);
   // (the kernels count a batch's steps in 32 bits)
   if ((target <= batch && !far) || steps * batch > INT_MAX) return s;

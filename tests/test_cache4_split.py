@@ -22,4 +22,6 @@ def test_a_long_sequence_is_cut_in_any_batch(B, heads, hd, dtype):
 def test_short_sequences_and_large_batches_are_not():
     assert _bytes(64, 1000) == 0 and _bytes(257, 131072) == 0
     assert _bytes(16, 131072, G=256, hkv=32) == 0        # many rows: the row kernel takes a sequence whole
+    # every sequence has a round of workgroups of its own
+    assert _bytes(20, 131072, G=256, hkv=32, dtype=1) == 0 and _bytes(20, 131072, G=240, hkv=32, dtype=1) > 0
     assert _bytes(256, 2**31 - 1) == 0                  # more steps in all than 32 bits count
