@@ -424,11 +424,11 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
     load_values(ts, max(page, 0));
   }
   int n = 0;                                  // steps of `pages` already requested
-  bool keys = false;                          // the wave had a key
+  int keys = 0;                               // more than 0: the wave had a key (one scalar maximum a step)
   for (int t = ts; t < te; t += KW) {
     // a page that the cache does not have: none of its keys count
     const int valid = page < 0 ? 0 : v.len - t * STEP;
-    keys |= valid > 0;
+    keys = max(keys, valid);
     if (++n == 64) {
       pages = pages_from(t + KW);
       asm volatile("" : "+v"(pages));         // waits for them here, not in every step
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
   if (t < v.steps1) t += (v.steps1 - t + KW - 1) / KW * KW;
   for (; t < t1; t += KW) {
     const int k0 = (t - v.steps1) * STEP, f0 = b * a.fstride + k0, valid = v.nfresh - k0;
-    keys = true;
+    keys = 1;
     // every fragment of the keys, then of the values, is requested before the
     // first is used; keys past the end read the last one's, masked below
     Frag<T> k[KF][2];
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(64 * NWAVE, CB == 1 && sizeof(T) == 2 ? 4 : CB == 4
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
     l_run[cb] = sum_groups(l_run[cb]);
-    m_run[cb] = fmaxf(m_run[cb], keys ? M_KEYS : M_NONE);
+    m_run[cb] = fmaxf(m_run[cb], keys > 0 ? M_KEYS : M_NONE);
   }
   if constexpr (KW == 1) {
 #pragma unroll
