@@ -1,0 +1,856 @@
+"""Performance cases of sampled responses that share a prompt: pages with reference counts, an 8-bit
+paged prompt cache with the attention that reads it, and sampling.
+
+A program that draws several responses to one prompt makes four kinds of calls.
+A *fork* lets the samples' block tables list the prompt's pages, plans their first own
+tokens (the prompt's last page, where it is not full, is copied for each of them) and
+copies the pages' bytes.  A *compact* call gives back what finished requests held and moves
+the pages in use to the front of the pool.  A *store* quantises rows of keys and
+values into their sequences' pages and reads them back as the values that they now stand
+for; an *attend* pass lets each sequence's response rows attend to its
+cached keys and to the fresh ones.  A *sample* call draws a token for every row of logits.
+
+The cache holds e4m3 values (sign, four exponent bits, three mantissa bits, at most 448) with one
+power-of-two scale for each block of 32 tokens and head, for its keys and for its values.  One page
+of one head is, in bytes (T tokens, D dimensions):
+  keys    [T][D]
+  values  [T / 8][D / 32][16][2][8]   8-token blocks; dimension u D/16 + 2 i + s of token t is at [i][u][s][t]
+  scales  [T / 32][2], 16 bytes       biased exponents (127 is one) of the keys, of the values
+
+Widths, vocabularies, prompt lengths and response lengths are those of the workloads
+(``synth/workloads.py``) and of the prompt sweep, single tokens, contexts up to 128 Ki keys
+and vocabularies of other sizes beside them.
+"""
+
+import math
+
+import torch
+
+own = False
+
+BLOCK = 32           # tokens per scale
+E_MIN, E_MAX = -15, 7
+
+
+# -- cases ---------------------------------------------------------------------------------------
+def _fork(name, prompts, samples, lo, hi, grow, page, heads, hd, planes, seed=0):
+    c = dict(kind="fork", prompts=prompts, samples=samples, len_lo=lo, len_hi=hi, grow=grow, page=page, heads=heads, hd=hd,
+             planes=planes, length_seed=seed)
+    return dict(c, name=name) if name else c
+
+
+def _compact(name, prompts, samples, lo, hi, done, page, heads, hd, planes, seed=0):
+    c = dict(kind="compact", prompts=prompts, samples=samples, len_lo=lo, len_hi=hi, done=done, page=page, heads=heads,
+             hd=hd, planes=planes, length_seed=seed)
+    return dict(c, name=name) if name else c
+
+
+def _store(name, dtype, batch, lo, hi, append, heads, hd, page, seed=0, transposed=True):
+    c = dict(kind="store", dtype=dtype, batch=batch, len_lo=lo, len_hi=hi, append=append, heads=heads, hd=hd, page=page,
+             length_seed=seed, transposed=transposed)
+    return dict(c, name=name) if name else c
+
+
+def _attend(name, dtype, batch, lo, hi, rows, fresh, hq, hkv, hd, page, seed=0, ragged=False):
+    c = dict(kind="attend", dtype=dtype, batch=batch, len_lo=lo, len_hi=hi, rows=rows, fresh=fresh, hq=hq, hkv=hkv,
+             hd=hd, page=page, length_seed=seed, ragged=ragged)
+    return dict(c, name=name) if name else c
+
+
+def _sample(name, dtype, rows, vocab, filters, spread, mask=True, pad=0):
+    c = dict(kind="sample", dtype=dtype, rows=rows, vocab=vocab, filters=filters, spread=spread, mask=mask, pad=pad)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # eight samples of one user's prompt begin: four key heads, every layer's pages
+        _fork("fork_one_prompt_x8", 1, 8, 1000, 1000, 8, 64, 4, 128, 28),
+        # sixteen samples of each prompt of the ragged serving batch begin a response of up to 256 tokens
+        _fork("fork_ragged16_x16", 16, 16, 681, 1971, 256, 64, 32, 128, 4, seed=176),
+        # a small pool after three of its twelve requests have finished
+        _compact("compact_small", 4, 3, 57, 513, 0.25, 32, 4, 64, 2),
+        # a large server's pool after half of the requests have finished, samples of shared prompts among them
+        _compact("compact_b512", 128, 4, 256, 4096, 0.5, 64, 4, 128, 8, seed=1),
+        # the next token of 16 sequences enters the cache
+        _store("store8_token_b16", "bf16", 16, 681, 1971, 1, 32, 128, 64, seed=176, transposed=False),
+        # the prompts of the ragged serving batch, as a refresh leaves one layer's keys and (transposed) values
+        _store("store8_prompt_ragged16", "bf16", 16, 681, 1971, 0, 32, 128, 64, seed=176),
+        # the next token of 16 sequences, four key heads of seven query heads each
+        _attend("token8_gqa_b16", "bf16", 16, 681, 1971, 1, False, 28, 4, 128, 64, seed=176),
+        # long contexts: four users of up to 128 Ki tokens
+        _attend("token8_long_b4", "bf16", 4, 70001, 131072, 1, False, 28, 4, 128, 256, seed=5),
+        # a cached denoising step of the ragged serving batch
+        _attend("step8_ragged16", "bf16", 16, 681, 1971, 256, True, 32, 32, 128, 64, seed=176),
+        # one row of one user, every filter: the smallest call
+        _sample("sample_row_v126464", "fp32", 1, 126464, "kpm", 3.0),
+        # the response rows of one denoising step, temperature and top-p
+        _sample("sample_step_v126464", "fp32", 256, 126464, "p", 2.0),
+        # the response rows of four sequences, each with settings of its own
+        _sample("sample_b4_v152064", "fp32", 2048, 152064, "mixed", 2.5),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    page = rng.choice([32, 64, 128, 256])
+    seed = rng.randint(0, 1 << 20)
+    u = rng.random()
+    if u < 0.14:
+        prompts = _log_int(rng, 1, 24)
+        lo = _log_int(rng, 1, 1500)
+        return _fork(None, prompts, _log_int(rng, 1, max(1, 200 // prompts)), lo, _log_int(rng, lo, 2000),
+                     _log_int(rng, 1, 300), page, rng.choice([1, 4, 7, 8]), rng.choice([64, 128]), rng.randint(1, 4), seed)
+    if u < 0.26:
+        prompts = _log_int(rng, 1, 100)
+        lo = _log_int(rng, 1, 1000)
+        return _compact(None, prompts, rng.randint(1, 5), lo, _log_int(rng, lo, 3000), rng.choice([0.0, 0.2, 0.5, 0.9]),
+                        page, rng.choice([1, 3, 4]), rng.choice([64, 128]), rng.randint(1, 6), seed)
+    if u < 0.44:
+        dtype, hd = rng.choice(["bf16", "bf16", "fp32"]), rng.choice([64, 128])
+        batch, heads = _log_int(rng, 1, 16), rng.choice([1, 4, 7, 8, 32])
+        lo = _log_int(rng, 1, 1000)
+        return _store(None, dtype, batch, lo, _log_int(rng, lo, 1900), rng.choice([0, 0, 1, 1, 7, 40, 256]), heads, hd, page,
+                      seed, rng.random() < 0.5)
+    hq, hkv = rng.choice([(32, 32), (28, 4), (16, 2), (7, 1), (8, 8), (4, 4), (12, 4)])
+    hd = rng.choice([64, 128, 128])
+    if u < 0.54:      # single tokens
+        batch = _log_int(rng, 1, 32)
+        lo = _log_int(rng, 1, 2000)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, max(lo, min(60000, 131072 * 4 // batch // hkv))), 1,
+                       rng.random() < 0.3, hq, hkv, hd, page, seed)
+    if u < 0.62:      # short blocks
+        batch = _log_int(rng, 1, 16)
+        lo = _log_int(rng, 1, 2000)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, 6000), rng.randint(2, 40), rng.random() < 0.7, hq, hkv,
+                       hd, page, seed, rng.random() < 0.5)
+    if u < 0.72:      # denoising steps
+        batch = _log_int(rng, 1, 12)
+        lo = _log_int(rng, 16, 1024)
+        return _attend(None, "bf16", batch, lo, _log_int(rng, lo, 1900), 8 * rng.randint(8, 32), True, hq, hkv, hd, page,
+                       seed, rng.random() < 0.3)
+    if u < 0.77:
+        batch = rng.randint(1, 4)
+        lo = _log_int(rng, 1, 200)
+        return _attend(None, "fp32", batch, lo, _log_int(rng, lo, 1000), rng.choice([1, 5, 32, 64]), rng.random() < 0.7, 4,
+                       rng.choice([1, 2, 4]), hd, page, seed, rng.random() < 0.5)
+    return _sample(None, rng.choice(["fp32", "fp32", "bf16", "fp16"]), _log_int(rng, 1, 1024),
+                   rng.choice([1024, 126464, 152064, _log_int(rng, 1001, 150000)]),
+                   rng.choice(["", "k", "p", "m", "kp", "kpm", "mixed"]), rng.choice([0.5, 1.0, 2.0, 3.0, 5.0]),
+                   rng.random() < 0.7, rng.choice([0, 0, 3, 64]))
+
+
+def _lengths(case):
+    """Lengths of the cached sequences or prompts, a function of the case alone."""
+    g = torch.Generator().manual_seed(1000 + case["length_seed"])
+    n = case["prompts"] if "prompts" in case else case["batch"]
+    lens = torch.randint(case["len_lo"], case["len_hi"] + 1, (n,), generator=g).tolist()
+    if n > 1:
+        lens[0], lens[-1] = case["len_hi"], case["len_lo"]
+    return lens
+
+
+def _resp_lengths(case):
+    if not case["ragged"]:
+        return None
+    g = torch.Generator().manual_seed(2000 + case["length_seed"])
+    r = torch.randint(1, case["rows"] + 1, (case["batch"],), generator=g).tolist()
+    r[0] = case["rows"]
+    return r
+
+
+def _fork_lengths(case):
+    """Kept prompt tokens and new tokens of every sample (sample-major behind the prompts)."""
+    g = torch.Generator().manual_seed(3000 + case["length_seed"])
+    keep = [n for n in _lengths(case) for _ in range(case["samples"])]
+    grow = torch.randint(1, case["grow"] + 1, (len(keep),), generator=g).tolist()
+    return keep, grow
+
+
+def _compact_lengths(case):
+    """Per request: prompt tokens, own tokens behind them, whether it is done.  The samples of a prompt share its pages."""
+    g = torch.Generator().manual_seed(4000 + case["length_seed"])
+    p = [n for n in _lengths(case) for _ in range(case["samples"])]
+    extra = torch.randint(0, 257, (len(p),), generator=g).tolist()
+    done = torch.zeros(len(p), dtype=torch.bool)
+    done[torch.randperm(len(p), generator=g)[:int(round(case["done"] * len(p)))]] = True
+    return p, extra, done.tolist()
+
+
+def _pages(n, page):
+    return (n + page - 1) // page
+
+
+def _page_bytes(page, hd):
+    return 2 * page * hd + 16
+
+
+def _store_rows(case):
+    """Start and rows of every sequence's store, and the positions that are valid afterwards and touched by it."""
+    lens = _lengths(case)
+    if case["append"]:
+        return [(n, case["append"]) for n in lens]
+    return [(0, n) for n in lens]
+
+
+def _compact_layout(case):
+    """Page numbers in the pool's order of use: rows of the table, counts, pages in all.  On the host."""
+    page = case["page"]
+    p, extra, done = _compact_lengths(case)
+    rows, refs, at = [], {}, 0
+    for i, (n, x) in enumerate(zip(p, extra)):
+        full = n // page
+        if i % case["samples"] == 0:
+            shared = list(range(at, at + full))
+            at += full
+        own_ = list(range(at, at + _pages(n + x, page) - full))
+        at += len(own_)
+        rows.append(shared + own_)
+    for r in rows:
+        for q in r:
+            refs[q] = refs.get(q, 0) + 1
+    return rows, refs, at
+
+
+def work(case):
+    kind, page = case["kind"], case.get("page")
+    if kind == "fork":
+        keep, grow = _fork_lengths(case)
+        copies = sum(1 for n in keep if n % page)
+        lens = _lengths(case)
+        taken = copies + sum(_pages(n + g, page) - _pages(n, page) for n, g in zip(keep, grow))
+        n_pages = sum(_pages(n, page) for n in lens) + taken + 7
+        # tables, counts in and out, slots out; the copied pages, read and written
+        small = 8 * sum(_pages(n, page) for n in keep) + 8 * n_pages + 4 * sum(grow) + 16 * len(keep)
+        return {"bytes": small + 2 * copies * case["heads"] * _page_bytes(page, case["hd"]) * case["planes"], "flops": 0}
+    if kind == "compact":
+        rows, refs, n = _compact_layout(case)
+        order = _compact_order(case, n)
+        done = _compact_lengths(case)[2]
+        for r, d in zip(rows, done):
+            for q in r if d else ():
+                refs[q] -= 1
+        used = [order[q] for q in range(n) if refs[q] > 0]
+        moves = sum(1 for q in used if q >= len(used))
+        small = 8 * sum(len(r) for r in rows) + 12 * (n + 9)
+        return {"bytes": small + 2 * moves * case["heads"] * _page_bytes(page, case["hd"]) * case["planes"], "flops": 0}
+    if kind == "store":
+        e = 2 if case["dtype"] == "bf16" else 4
+        rows = sum(c for _, c in _store_rows(case))
+        back = sum(s + c - s // BLOCK * BLOCK for s, c in _store_rows(case))
+        per = 2 * case["heads"] * case["hd"]
+        # rows in, codes out; what a joined block holds already in and out; codes in, values out
+        return {"bytes": per * (rows * (e + 1) + 2 * (back - rows) + back * (1 + e)) + 4 * back, "flops": 0}
+    if kind == "sample":
+        e = 4 if case["dtype"] == "fp32" else 2
+        n = case["rows"] * case["vocab"]
+        return {"bytes": e * n + 28 * case["rows"], "flops": n}      # an exponential counts as one operation
+    lens, resp = _lengths(case), _resp_lengths(case)
+    resp = resp or [case["rows"]] * case["batch"]
+    e = 2 if case["dtype"] == "bf16" else 4
+    hq, hkv, hd = case["hq"], case["hkv"], case["hd"]
+    fresh = resp if case["fresh"] else [0] * case["batch"]
+    by = sum(r * hq * hd * 2 * e + 2 * hkv * hd * e * f + 2 * hkv * (hd * n + _pages(n, BLOCK)) + 4 * _pages(n, page) + 4
+             for n, r, f in zip(lens, resp, fresh))
+    return {"bytes": by, "flops": sum(4 * r * (n + f) * hq * hd for n, r, f in zip(lens, resp, fresh))}
+
+
+# -- inputs --------------------------------------------------------------------------------------
+def _dtype(case):
+    return {"bf16": torch.float16, "fp32": torch.float32}[case["dtype"]]
+
+
+def _keys(shape, g):
+    """Rows of keys or values: normal, a few dimensions much larger than the others, as rotated keys have them."""
+    x = torch.randn(shape, generator=g, device="cuda")
+    wide = torch.rand(shape[-1], generator=g, device="cuda") < 0.05
+    return x * torch.where(wide, 4.0, 1.0)
+
+
+def _table(lens, page, spare, g):
+    """Block table over pages in random order."""
+    need = [_pages(n, page) for n in lens]
+    n_pages = sum(need) + spare
+    order = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), max(max(need), 1)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, n_pages
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _compact_order(case, n):
+    g = torch.Generator().manual_seed(5000 + case["length_seed"])
+    return torch.randperm(n + 9, generator=g).tolist()
+
+
+def _pool_data(case, n_pages, g):
+    """Bytes of a pool's pages, one plane per layer.  Bytes of any kind: the calls move them as they are."""
+    shape = (case["planes"], n_pages, case["heads"], _page_bytes(case["page"], case["hd"]))
+    return torch.randint(0, 256, shape, generator=g, dtype=torch.uint8, device="cuda")
+
+
+def _prepare_fork(case, s, g):
+    page, lens = case["page"], _lengths(case)
+    keep, grow = _fork_lengths(case)
+    P, N = len(lens), len(keep)
+    have = [_pages(n, page) for n in lens]
+    taken = sum(1 for n in keep if n % page) + sum(_pages(n + x, page) - _pages(n, page) for n, x in zip(keep, grow))
+    n_pages = sum(have) + taken + 7
+    width = max(_pages(n + x, page) for n, x in zip(keep, grow)) + 2
+    order = torch.randperm(n_pages, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((P + N, width), -1, dtype=torch.int32, device="cuda")
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(have):
+        table[b, :n] = order[at:at + n]
+        at += n
+    refs[order[:at].long()] = 1
+    head, rest = int(torch.randint(0, n_pages, (1,), generator=g, device="cuda")), n_pages - at
+    free = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    free[(head + torch.arange(rest, device="cuda")) % n_pages] = order[at:]
+    s.update(table=table, table2=torch.empty_like(table), refs=refs, free=free, n_pages=n_pages, pool=_i32([head, rest]),
+             src=_i32([i // case["samples"] for i in range(N)]), dst=_i32(list(range(P, P + N))), keep=_i32(keep),
+             old=_i32(lens + keep), new=_i32(lens + [n + x for n, x in zip(keep, grow)]),
+             rows=(sum(grow) + 63) // 64 * 64 + 64, data=_pool_data(case, n_pages, g))
+
+
+def _prepare_compact(case, s, g):
+    page = case["page"]
+    p, extra, done = _compact_lengths(case)
+    rows, refs, n = _compact_layout(case)
+    order = _compact_order(case, n)
+    n_pages = n + 9
+    width = max(len(r) for r in rows) + 1
+    at, rest = int(torch.randint(0, n_pages, (1,), generator=g, device="cuda")), order[n:]
+    table = torch.tensor([[order[q] for q in r] + [-1] * (width - len(r)) for r in rows], dtype=torch.int32)
+    count = torch.zeros(n_pages, dtype=torch.int32)
+    count[torch.tensor([order[q] for q in refs])] = torch.tensor(list(refs.values()), dtype=torch.int32)
+    free = torch.zeros(n_pages, dtype=torch.int32)
+    free[(at + torch.arange(len(rest))) % n_pages] = torch.tensor(rest, dtype=torch.int32)
+    s.update(table=table.cuda(), table2=torch.empty_like(table).cuda(), refs=count.cuda(), free=free.cuda(),
+             n_pages=n_pages, pool=_i32([at, len(rest)]), old=_i32([a + b for a, b in zip(p, extra)]),
+             new=_i32([0 if d else a + b for a, b, d in zip(p, extra, done)]), rows=0, data=_pool_data(case, n_pages, g))
+
+
+def _prepare_store(case, s, g):
+    page, hd, heads = case["page"], case["hd"], case["heads"]
+    spans = _store_rows(case)
+    table, n_pages = _table([a + c for a, c in spans], page, 3, g)
+    data = torch.zeros(n_pages, heads, _page_bytes(page, hd), dtype=torch.uint8, device="cuda")
+    _fill(data, page, hd, g)
+    n = sum(c for _, c in spans)
+    rows = n + 5          # rows behind the last sequence's: not stored
+    k = _keys((heads, rows, hd), g).to(_dtype(case))
+    v = _keys((heads, rows, hd), g).to(_dtype(case))
+    off = [0]
+    for _, c in spans:
+        off.append(off[-1] + c)
+    # slots of every token that the touched blocks then hold
+    slots = []
+    for b, (a, c) in enumerate(spans):
+        pos = torch.arange(a // BLOCK * BLOCK, a + c, device="cuda")
+        slots.append(table[b, pos // page] * page + pos % page)
+    s.update(data=data, n_pages=n_pages, table=table, start=_i32([a for a, _ in spans]), off=_i32(off),
+             slots=torch.cat(slots).to(torch.int32), k=k, lut=_lut("cuda"), spans=spans,
+             # the values as the prompt cache holds them: transposed, seen row by row
+             v=v.transpose(1, 2).contiguous().transpose(1, 2) if case["transposed"] else v)
+
+
+def _prepare_attend(case, s, g):
+    page, hd, heads = case["page"], case["hd"], case["hkv"]
+    lens = _lengths(case)
+    table, n_pages = _table(lens, page, 3, g)
+    data = torch.zeros(n_pages, heads, _page_bytes(page, hd), dtype=torch.uint8, device="cuda")
+    _fill(data, page, hd, g)
+    G, B = case["rows"], case["batch"]
+    pad = (G + 7) // 8 * 8
+    s.update(data=data, table=table, lens=_i32(lens), lut=_lut("cuda"),
+             q=(torch.randn(case["hq"], B * G, hd, generator=g, device="cuda") * 2).to(_dtype(case)),
+             max_cached=max(lens), stride=pad, k2=None, vt2=None, resp=None,
+             out=torch.zeros(B * G, case["hq"] * hd, device="cuda",
+                             dtype=torch.bfloat16 if case["dtype"] == "bf16" else torch.float32))
+    if case["fresh"]:
+        ld = (B * pad + 63) // 64 * 64
+        s["k2"] = _keys((heads, ld, hd), g).to(_dtype(case))
+        s["vt2"] = _keys((heads, hd, ld), g).to(_dtype(case))
+    resp = _resp_lengths(case)
+    if resp:
+        s["resp"] = _i32(resp)
+
+
+def _prepare_sample(case, s, g):
+    R, V = case["rows"], case["vocab"]
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[case["dtype"]]
+    # a language model's rows: a normal bulk, a few tokens far above it, some rows sure of one token
+    z = torch.randn(R, V + case["pad"], generator=g, device="cuda") * case["spread"]
+    top = torch.randint(0, V, (R, 12), generator=g, device="cuda")
+    z.scatter_add_(1, top, torch.rand(R, 12, generator=g, device="cuda") * 12)
+    sure = torch.rand(R, 1, generator=g, device="cuda") < 0.3
+    z[torch.arange(R, device="cuda"), top[:, 0]] += torch.where(sure[:, 0], 12.0, 0.0)
+    z = z.to(t)[:, :V]
+    u = lambda: torch.rand(R, generator=g, device="cuda")  # noqa: E731
+    f, each = case["filters"], case["filters"] == "mixed"
+    s.update(logits=z, u=u(), exclude=V - 1 if case["mask"] else -1, temperature=0.3 + 1.2 * u(), top_k=None, top_p=None,
+             min_p=None)
+    on = lambda x, off: torch.where(u() < 0.5, x, torch.full_like(x, off)) if each else x  # noqa: E731
+    if each or "k" in f:
+        s["top_k"] = on((torch.exp(u() * math.log(200)) + 1).to(torch.int32), 0)
+    if each or "p" in f:
+        s["top_p"] = on(0.5 + 0.49 * u(), 1.0)
+    if each or "m" in f:
+        s["min_p"] = on(torch.exp(-1.5 - 5 * u()), 0.0)
+    if each:        # some rows are not drawn: the largest logit
+        s["temperature"] = torch.where(u() < 0.1, 0.0, s["temperature"])
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s = dict(case=case)
+    {"fork": _prepare_fork, "compact": _prepare_compact, "store": _prepare_store, "attend": _prepare_attend,
+     "sample": _prepare_sample}[case["kind"]](case, s, g)
+    return s
+
+
+# -- the plain forms -----------------------------------------------------------------------------
+def _power(e):
+    """2^e of whole numbers e in 64 bits, exactly."""
+    return torch.tensor([2.0 ** k for k in range(-160, 161)], dtype=torch.float64, device=e.device)[e.long() + 160]
+
+
+def _lut(dev):
+    """The 256 values of e4m3."""
+    c = torch.arange(256, device=dev)
+    e, m = (c >> 3) & 15, (c & 7).double()
+    x = torch.where(e == 0, m * 2.0 ** -9, (1 + m / 8) * _power(e - 7))
+    x = torch.where((c & 127) == 127, math.nan, x)
+    return torch.where(c >= 128, -x, x).float()
+
+
+def _two_to(e):
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
+
+
+def _scale_of(top):
+    """Least e with top <= 448 * 2^e, clamped."""
+    m, e = torch.frexp(top)
+    e = torch.where(m > 0.875, e - 8, e - 9)
+    return torch.where(top == 0, torch.full_like(e, E_MIN), e).clamp(E_MIN, E_MAX)
+
+
+def _codes(x, e):
+    """e4m3 codes of x / 2^e: nearest, ties to even, saturating.  Every operation here is exact in 32 bits."""
+    y = (x.abs() * _two_to(-e)).clamp(max=448.0)
+    b = torch.where(y == 0, -6, (torch.frexp(y).exponent - 1).clamp(min=-6))     # of the normal numbers, or of the smallest
+    n = torch.round(y * _two_to(3 - b))                       # steps of 2^(b - 3), up to 16
+    code = (8 * (b + 6) + n.to(b.dtype)).to(torch.uint8)      # 16 steps carry into the exponent
+    return code + 128 * torch.signbit(x).to(torch.uint8)
+
+
+def _parts(data, page, D):
+    """Views of page bytes [...][page bytes]: keys [...][T][D], values [...][T/8][D/32][16][2][8], scales [...][T/32][2]."""
+    k, v, sc = data.split([page * D, page * D, 16], -1)
+    return (k.unflatten(-1, (page, D)), v.unflatten(-1, (page // 8, D // 32, 16, 2, 8)),
+            sc[..., :page // BLOCK * 2].unflatten(-1, (page // BLOCK, 2)))
+
+
+def _value_rows(v):
+    """[...][T/8][D/32][16][2][8] -> [...][T][D]: dimension (u, i, s) of token (block, t)."""
+    return v.movedim(-1, -4).transpose(-3, -2).flatten(-3).flatten(-3, -2)
+
+
+def _value_blocks(x):
+    """[...][T][D] -> [...][T/8][D/32][16][2][8]."""
+    T, D = x.shape[-2:]
+    return x.unflatten(-1, (16, D // 32, 2)).unflatten(-4, (T // 8, 8)).transpose(-3, -2).movedim(-4, -1)
+
+
+def _fill(data, page, hd, g):
+    """Every page full of stored keys and values."""
+    n, heads, _ = data.shape
+    for a in range(0, n, 256):
+        d = data[a:a + 256]
+        k, v, sc = _parts(d, page, hd)
+        for i, (dst, put) in enumerate(((k, lambda x: x), (v, _value_blocks))):
+            x = _keys((d.shape[0], heads, page, hd), g)
+            e = _scale_of(x.abs().unflatten(2, (-1, BLOCK)).amax((-1, -2)))
+            dst.copy_(put(_codes(x, e.repeat_interleave(BLOCK, 2)[..., None])))
+            sc[..., i] = (e + 127).to(torch.uint8)
+
+
+def _before(x):
+    return x.cumsum(0) - x
+
+
+def _plan_plain(s, table, refs):
+    """The plan with reference counts; s["free"] changes in place.  Pages of row b: its first _pages(length) entries."""
+    page, old, new, n = s["case"]["page"], s["old"].long(), s["new"].long(), s["n_pages"]
+    B, width = table.shape
+    have, want = _pages(old, page), _pages(new, page)
+    j = torch.arange(width, device="cuda")[None]
+    row = torch.arange(B, device="cuda")
+    entry = table.long().clamp(0, n - 1)
+    drop = (j >= want[:, None]) & (j < have[:, None])
+    at = torch.where(drop, entry, n).flatten()
+    r = torch.cat([refs.long(), refs.new_zeros(1).long()])
+    r = r.scatter_add(0, at, torch.full_like(at, -1))
+    # the last row that drops a page gives it back
+    last = torch.full_like(r, -1).scatter_reduce(0, at, row[:, None].expand(B, width).flatten(), "amax")
+    back = drop & (r[entry] == 0) & (last[entry] == row[:, None])
+    # rows that grow from inside a page
+    tail = torch.where((new > old) & (old % page != 0), entry.gather(1, (have - 1).clamp(min=0)[:, None])[:, 0], n)
+    writers = torch.zeros_like(r).scatter_add(0, tail, torch.ones_like(tail))
+    lastw = torch.full_like(r, -1).scatter_reduce(0, tail, row, "amax")
+    cow = (tail < n) & (r[tail] > 1) & ~((writers[tail] == r[tail]) & (lastw[tail] == row))
+    r = r.scatter_add(0, torch.where(cow, tail, n), torch.full_like(tail, -1))
+    # pages taken: the copy first
+    grow = (want - have).clamp(min=0)
+    takes = cow.long() + grow
+    head, count = s["pool"][0].long(), s["pool"][1].long()
+    first = _before(takes)
+    from_ring = lambda i: s["free"][(head + i) % n]  # noqa: E731
+    cow_to = torch.where(cow, from_ring(first), -1)
+    is_copy = cow[:, None] & (j == have[:, None] - 1)
+    is_new = (j >= have[:, None]) & (j < want[:, None])
+    page_in = from_ring((first + cow.long())[:, None] + j - have[:, None])
+    out = torch.where(is_new, page_in, torch.where(is_copy, cow_to[:, None].to(table.dtype), table))
+    r[:n] = torch.where(torch.zeros(n + 1, dtype=torch.bool, device="cuda").scatter(
+        0, torch.where(is_copy | is_new, out.long(), n).flatten(), True)[:n], 1, r[:n])
+    nback = back.sum(1)
+    place = _before(nback)[:, None] + back.long().cumsum(1) - 1
+    to = torch.where(back, (head + count + place) % n, n).flatten()
+    s["free"].copy_(torch.cat([s["free"], s["free"][:1]]).scatter(0, to, table.flatten())[:n])
+    ntake, ngive = takes.sum(), nback.sum()
+    pool = torch.stack([(head + ntake) % n, count - ntake + ngive]).to(torch.int32)
+    rows = (new - old).clamp(min=0)
+    off = torch.cat([rows.new_zeros(1), rows.cumsum(0)])
+    t = torch.arange(s["rows"], device="cuda")
+    b = torch.searchsorted(off[1:], t, right=True).clamp(max=B - 1)
+    p = old[b] + t - off[b]
+    slots = torch.where(t < off[-1], out[b, (p // page).clamp(0, width - 1)] * page + p % page, -1).to(torch.int32)
+    short = (ntake > count).to(torch.int32).reshape(1)
+    return dict(table=out, refs=r[:n].to(torch.int32), pool=pool, row_off=off.to(torch.int32), slots=slots,
+                copy_src=torch.where(cow, tail, -1).to(torch.int32), copy_dst=cow_to.to(torch.int32), status=short)
+
+
+def _copy_plain(data, src, dst):
+    ok = src >= 0
+    data[:, dst[ok].long()] = data[:, src[ok].long()]
+
+
+def _fork_plain(s):
+    c, table, n = s["case"], s["table"], s["n_pages"]
+    j = torch.arange(table.shape[1], device="cuda")[None]
+    held = j < _pages(s["keep"], c["page"])[:, None]
+    rows = table[s["src"].long()]
+    table[s["dst"].long()] = torch.where(held, rows, table[s["dst"].long()])
+    at = torch.where(held, rows.long(), n).flatten()
+    refs = torch.cat([s["refs"], s["refs"][:1]]).scatter_add(0, at, torch.ones_like(at, dtype=torch.int32))[:n]
+    out = _plan_plain(s, table, refs)
+    _copy_plain(s["data"], out["copy_src"], out["copy_dst"])
+    return dict(out, forked=table, free=s["free"], data=s["data"])
+
+
+def _compact_plain(s):
+    page, n = s["case"]["page"], s["n_pages"]
+    out = _plan_plain(s, s["table"], s["refs"])
+    refs, table = out["refs"], out["table"]
+    used = refs > 0
+    i = torch.arange(n, device="cuda")
+    U = used.sum()
+    hi, lo = used & (i >= U), ~used & (i < U)
+    half = n // 2
+    pick = lambda m: torch.full((half + 1,), -1, dtype=torch.int32, device="cuda").scatter(  # noqa: E731
+        0, torch.where(m, m.long().cumsum(0) - 1, half), i.to(torch.int32))[:half]
+    src, dst = pick(hi), pick(lo)
+    where_ = torch.where(hi, dst[(hi.long().cumsum(0) - 1).clamp(0, max(half - 1, 0))].long(), i)
+    j = torch.arange(table.shape[1], device="cuda")[None]
+    held = j < _pages(s["new"], page)[:, None]
+    table = torch.where(held, where_[table.long().clamp(0, n - 1)].to(torch.int32), table)
+    refs2 = torch.where(i < U, torch.where(lo, 0, refs), 0)
+    refs2 = torch.cat([refs2, refs2[:1]]).scatter(0, torch.where(hi, where_, n), torch.where(hi, refs, 0))[:n]
+    free = torch.where(i < n - U, U + i, -1).to(torch.int32)
+    _copy_plain(s["data"], src, dst)
+    return dict(pool=torch.stack([torch.zeros_like(U), n - U]).to(torch.int32), free=free, table=table,
+                refs=refs2.to(torch.int32), move_src=src, move_dst=dst, moves=hi.sum().to(torch.int32).reshape(1),
+                data=s["data"])
+
+
+def _store_plain(s):
+    c = s["case"]
+    page, hd = c["page"], c["hd"]
+    k, v, sc = _parts(s["data"], page, hd)
+    # every touched block: its sequence, number and row of its first token
+    seq, blk = [], []
+    for b, (a, n) in enumerate(s["spans"]):
+        m = torch.arange(a // BLOCK, (a + n - 1) // BLOCK + 1, device="cuda")
+        blk.append(m)
+        seq.append(torch.full_like(m, b))
+    seq, blk = torch.cat(seq), torch.cat(blk)
+    start, off = s["start"].long(), s["off"].long()
+    pos = blk[:, None] * BLOCK + torch.arange(BLOCK, device="cuda")
+    row = off[seq][:, None] + pos - start[seq][:, None]
+    new = (pos >= start[seq][:, None]) & (row < off[seq + 1][:, None])
+    held = pos < start[seq][:, None]
+    pg, o = s["table"][seq, blk * BLOCK // page].long(), blk * BLOCK % page
+    joined = held[:, 0][:, None]
+    at = o[:, None] + torch.arange(BLOCK, device="cuda")
+    vb = torch.arange(BLOCK // 8, device="cuda") + (o // 8)[:, None]
+    src = row.clamp(0, s["k"].shape[1] - 1)
+    for i, x in ((0, s["k"]), (1, s["v"])):
+        x = x[:, src].float().transpose(0, 1)                              # [blocks][heads][32][D]
+        x = torch.where(new[:, None, :, None], x, 0.0)
+        was = sc[pg, :, o // BLOCK, i].to(torch.int32) - 127               # [blocks][heads]
+        stored = k[pg[:, None], :, at] if i == 0 else v[pg[:, None], :, vb]
+        stored = stored.transpose(1, 2) if i == 0 else _value_rows(stored.transpose(1, 2))
+        e = _scale_of(x.abs().amax((-1, -2)))
+        e = torch.where(joined, torch.maximum(e, was), e)
+        whole = torch.where(held[:, None, :, None], s["lut"][stored.int()] * _two_to(was)[..., None, None], x)
+        code = _codes(whole, e[..., None, None])
+        code = torch.where((held | new)[:, None, :, None], code, stored)
+        if i == 0:
+            k[pg[:, None], :, at] = code.transpose(1, 2)
+        else:
+            v[pg[:, None], :, vb] = _value_blocks(code).transpose(1, 2)
+        sc[pg, :, o // BLOCK, i] = (e + 127).to(torch.uint8)
+    # back again: the values that the tokens of these blocks stand for
+    p, o = s["slots"].long() // page, s["slots"].long() % page
+    e = _two_to(sc[p, :, o // BLOCK].int() - 127)                          # [rows][heads][2]
+    kk = s["lut"][k[p, :, o].int()] * e[..., 0, None]
+    vv = v[p, :, o // 8, :, :, :, o % 8]                                   # [rows][heads][D/32][16][2]
+    vv = s["lut"][vv.transpose(-3, -2).flatten(-3).int()] * e[..., 1, None]
+    return {n: x.transpose(0, 1).to(_dtype(c)).contiguous() for n, x in (("k", kk), ("v", vv))}
+
+
+def _attend_plain(s):
+    c = s["case"]
+    page, hd, hkv, B, G = c["page"], c["hd"], c["hkv"], c["batch"], c["rows"]
+    k, v, sc = _parts(s["data"][s["table"].clamp(min=0).long()], page, hd)            # [B][pages][heads][...]
+    e = _two_to(sc.int() - 127).repeat_interleave(BLOCK, -2)                          # [B][pages][heads][T][2]
+    k = s["lut"][k.int()] * e[..., 0, None]
+    v = s["lut"][_value_rows(v).int()] * e[..., 1, None]
+    k, v = (t.transpose(1, 2).flatten(2, 3)[:, :, :s["max_cached"]] for t in (k, v))
+    ok = torch.arange(k.shape[2], device="cuda")[None] < s["lens"][:, None]
+    n_resp = s["resp"] if s["resp"] is not None else torch.full_like(s["lens"], G)
+    if c["fresh"]:
+        cut = lambda t: t[:, :B * s["stride"]].float().view(hkv, B, s["stride"], hd)[:, :, :G].transpose(0, 1)  # noqa: E731
+        k, v = torch.cat([k, cut(s["k2"])], 2), torch.cat([v, cut(s["vt2"].transpose(1, 2).contiguous())], 2)
+        ok = torch.cat([ok, torch.arange(G, device="cuda")[None] < n_resp[:, None]], 1)
+    q = s["q"].float().view(hkv, -1, B, G, hd).permute(2, 0, 1, 3, 4).reshape(B, hkv, -1, hd)
+    z = torch.matmul(q, k.transpose(2, 3).contiguous()) / math.sqrt(hd)
+    z = z.masked_fill(~ok[:, None, None], -math.inf)
+    m = z.amax(-1, keepdim=True).clamp(min=-3e38)       # a row without keys gives zeros
+    p = torch.exp(z - m)
+    o = torch.matmul(p, v) / p.sum(-1, keepdim=True).clamp(min=1e-38)
+    o = o.view(B, hkv, -1, G, hd).permute(0, 3, 1, 2, 4).reshape(B, G, -1)
+    o = torch.where((torch.arange(G, device="cuda")[None] < n_resp[:, None])[..., None], o, 0.0)
+    return o.reshape(B * G, -1).to(s["out"].dtype)
+
+
+def _sample_plain(s):
+    """Row by row: the order of falling logits, its prefix that the filters keep, the draw in the vocabulary's order.
+    Sums over the vocabulary in 64 bits: the drawn token changes where one of them does."""
+    R, V = s["logits"].shape
+    off = lambda x, d, t: torch.full((R,), d, dtype=t, device="cuda") if x is None else x  # noqa: E731
+    top_k, top_p = off(s["top_k"], 0, torch.int32), off(s["top_p"], 1.0, torch.float32)
+    min_p = off(s["min_p"], 0.0, torch.float32)
+    token, logp = [], []
+    for a in range(0, R, 128):
+        at = slice(a, min(a + 128, R))
+        z = s["logits"][at].double()
+        if s["exclude"] >= 0:
+            z[:, s["exclude"]] = -math.inf
+        t = s["temperature"][at].double()[:, None]
+        z, order = torch.sort(z, stable=True, dim=-1, descending=True)
+        w = torch.exp((z - z[:, :1]) / torch.where(t > 0, t, 1.0))
+        i = torch.arange(V, device="cuda")[None]
+        k = top_k[at].long()[:, None]
+        keep = (i < torch.where(k > 0, k, V)) & (t > 0)
+        w1 = torch.where(keep, w, 0.0)
+        before = w1.cumsum(-1) - w1
+        p = top_p[at].double()[:, None]
+        keep &= (p >= 1) | (before < p * w1.sum(-1, keepdim=True))
+        keep &= w >= min_p[at].double()[:, None]
+        keep[:, 0] = True
+        w = torch.where(keep, w, 0.0)
+        w = torch.zeros_like(w).scatter(1, order, w)
+        total = w.sum(-1, keepdim=True)
+        drawn = (w.cumsum(-1) <= s["u"][at].double()[:, None] * total).sum(-1)
+        drawn = torch.minimum(drawn, (V - 1) - (w > 0).flip(-1).int().argmax(-1))
+        token.append(drawn.to(torch.int32))
+        logp.append((torch.log(w.gather(1, drawn[:, None])) - torch.log(total))[:, 0].float())
+    return {"token": torch.cat(token), "logp": torch.cat(logp)}
+
+
+def run(s):
+    c = s["case"]
+    if not own:
+        return {"fork": _fork_plain, "compact": _compact_plain, "store": _store_plain, "attend": _attend_plain,
+                "sample": _sample_plain}[c["kind"]](s)
+    from paper_2608_08086_amd import archer
+    if c["kind"] == "sample":
+        token, logp = archer.op_sample(s["logits"], s["u"], temperature=s["temperature"], top_k=s["top_k"],
+                                       top_p=s["top_p"], min_p=s["min_p"], exclude=s["exclude"])
+        return {"token": token, "logp": logp}
+    if c["kind"] in ("fork", "compact"):
+        table, refs = s["table"], s["refs"]
+        if c["kind"] == "fork":
+            refs, _ = archer.pages_fork(s["src"], s["dst"], s["keep"], c["page"], table, refs)
+        p = archer.pages_plan(s["old"], s["new"], c["page"], table, s["free"], s["pool"], refs, s["rows"],
+                              table_out=s["table2"])
+        if c["kind"] == "fork":
+            archer.pages_copy(s["data"], p.copy_src, p.copy_dst)
+            return dict(p._asdict(), forked=table, free=s["free"], data=s["data"])
+        m = archer.pages_compact(s["new"], c["page"], p.table, p.refs)
+        archer.pages_copy(s["data"], m.move_src, m.move_dst)
+        return dict(m._asdict(), data=s["data"])
+    cache = archer.Cache8(s["data"], c["page"], c["hd"])
+    if c["kind"] == "store":
+        archer.cache8_write(cache, s["table"], s["start"], s["off"], s["k"], s["v"])
+        k, v = archer.cache8_read(cache, s["slots"], _dtype(c))
+        return {"k": k, "v": v}
+    return archer.op_attention_cache8(s["q"], cache, s["table"], s["lens"], s["max_cached"], K2=s["k2"], Vt2=s["vt2"],
+                                      fresh_stride=s["stride"], resp_len=s["resp"], O=s["out"])
+
+
+# -- the definition in 64 bits -------------------------------------------------------------------
+def _nearest(x, e):
+    """The e4m3 value nearest to x / 2^e, times 2^e, in 64 bits: ties to even, at most 448."""
+    scale = _power(e)
+    y = x.abs() / scale
+    step = torch.full_like(y, 2.0 ** -9)
+    for b in range(-5, 9):
+        step = torch.where(y >= 2.0 ** b, 2.0 ** (b - 3), step)
+    r = torch.floor(y / step)
+    rest = y / step - r
+    r = torch.where((rest > 0.5) | ((rest == 0.5) & (r % 2 == 1)), r + 1, r)
+    return torch.copysign((r * step).clamp(max=448.0) * scale, x)
+
+
+def _least_exponent(top):
+    e = torch.full_like(top, E_MIN)
+    for k in range(E_MIN, E_MAX):
+        e = torch.where(top > 448 * 2.0 ** k, k + 1.0, e)
+    return e
+
+
+def _token(data, page, D, pages, at):
+    """Keys and values of one sequence, token by token from their bytes [n][heads][n bytes]: [heads][n][D] in 64 bits,
+    and their exponents [heads][n]."""
+    d = data[pages]
+    n, H, _ = d.shape
+    dim = torch.arange(D, device=d.device)
+    unit, inside = dim // (D // 16), dim % (D // 16)
+    a = at[:, None]
+    k_at = a * D + dim
+    v_at = page * D + (a // 8 * (D // 32) + inside // 2) * 256 + unit * 16 + inside % 2 * 8 + a % 8
+    out = []
+    for i, c_at in enumerate((k_at, v_at)):
+        c = torch.gather(d, 2, c_at[:, None].expand(n, H, D)).long()
+        ex, m = c // 8 % 16, (c % 8).double()
+        x = torch.where(ex == 0, m / 512, (8 + m) * _power(ex - 10))
+        x = torch.where(c >= 128, -x, x)
+        s_at = (2 * page * D + at // 32 * 2 + i)[:, None, None].expand(n, H, 1)
+        e = torch.gather(d, 2, s_at)[..., 0].double() - 127
+        out.append(((x * _power(e)[..., None]).transpose(0, 1), e.T))
+    return out
+
+
+def _exact_store(case, s):
+    page, hd = case["page"], case["hd"]
+    out, at = {"k": [], "v": []}, 0
+    for b, (a, n) in enumerate(s["spans"]):
+        a0 = a // BLOCK * BLOCK
+        pos = torch.arange(a0, max(a, a0 + 1), device="cuda")
+        old = _token(s["data"], page, hd, s["table"][b, pos // page].long(), pos % page)
+        for name, (was, e_was), x in (("k", old[0], s["k"]), ("v", old[1], s["v"])):
+            rows = torch.cat([was[:, :a - a0], x[:, at:at + n].double()], 1)
+            for i in range(0, rows.shape[1], BLOCK):
+                blk = rows[:, i:i + BLOCK]
+                new = blk[:, a - a0:] if i == 0 else blk
+                e = _least_exponent(new.abs().amax((1, 2)))
+                if i == 0 and a > a0:
+                    e = torch.maximum(e, e_was[:, 0])
+                out[name].append(_nearest(blk, e[:, None, None]))
+        at += n
+    return {k: torch.cat(v, 1) for k, v in out.items()}
+
+
+def _exact_sample(s):
+    """Every row for itself, without a sort of the row: the filters by thresholds on the logit, ties by index."""
+    R, V = s["logits"].shape
+    get = lambda n, r, d: d if s[n] is None else s[n][r].item()  # noqa: E731
+    token, logp = torch.zeros(R, dtype=torch.int32), torch.zeros(R, dtype=torch.float64)
+    allowed = torch.ones(V, dtype=torch.bool, device="cuda")
+    if s["exclude"] >= 0:
+        allowed[s["exclude"]] = False
+    for r in range(R):
+        z = torch.where(allowed, s["logits"][r].double(), -math.inf)
+        t, k, p, mp = s["temperature"][r].item(), get("top_k", r, 0), get("top_p", r, 1.0), get("min_p", r, 0.0)
+        top = z.max()
+        best = int((z == top).int().argmax())
+        if t <= 0:
+            token[r] = best
+            continue
+        w = torch.exp((z - top) / t)
+
+        def first(keep, count):
+            """The first `count` of keep in the order of falling logits and rising indexes."""
+            zz = torch.where(keep, z, -math.inf)
+            edge = torch.topk(zz, count).values[-1]
+            above, ties = keep & (z > edge), keep & (z == edge)
+            return above | (ties & (ties.cumsum(0) <= count - above.sum()))
+
+        keep = z > -math.inf
+        if k > 0:
+            keep = first(keep, min(k, int(keep.sum())))
+        if p < 1:
+            v = torch.where(keep, z, -math.inf)
+            vals = torch.topk(v, int(keep.sum())).values
+            mass = torch.exp((vals - top) / t).cumsum(0)
+            keep = first(keep, int((mass < p * mass[-1]).sum().clamp(max=len(mass) - 1)) + 1)
+        keep &= w >= mp
+        keep[best] = True
+        mass = torch.where(keep, w, 0.0).cumsum(0)
+        i = int(torch.searchsorted(mass, s["u"][r].double() * mass[-1], right=True))
+        if i >= V:
+            i = int(((w > 0) & keep).nonzero()[-1])
+        token[r], logp[r] = i, torch.log(w[i] / mass[-1]).cpu()
+    return {"token": token.cuda(), "logp": logp.cuda()}
+
+
+def exact(case, seed):
+    if case["kind"] in ("fork", "compact"):
+        return None
+    s = prepare(case, seed)
+    page = case.get("page")
+    if case["kind"] == "store":
+        return _exact_store(case, s)
+    if case["kind"] == "sample":
+        return _exact_sample(s)
+    B, G, hkv, grp, hd = case["batch"], case["rows"], case["hkv"], case["hq"] // case["hkv"], case["hd"]
+    resp = _resp_lengths(case) or [G] * B
+    out = torch.zeros(B * G, case["hq"] * hd, dtype=torch.float64, device="cuda")
+    for b, n in enumerate(_lengths(case)):
+        r = resp[b]
+        for h in range(hkv):
+            pos = torch.arange(n, device="cuda")
+            (k, _), (v, _) = _token(s["data"][:, h:h + 1], page, hd, s["table"][b, pos // page].long(), pos % page)
+            k, v = k[0], v[0]
+            if case["fresh"]:
+                at = slice(b * s["stride"], b * s["stride"] + r)
+                k = torch.cat([k, s["k2"][h, at].double()])
+                v = torch.cat([v, s["vt2"][h, :, at].double().T])
+            q = s["q"][h * grp:(h + 1) * grp, b * G:b * G + r].double().reshape(-1, hd)
+            p = torch.softmax(q @ k.T.contiguous() / math.sqrt(hd), -1)
+            o = (p @ v).view(grp, r, hd).transpose(0, 1).reshape(r, -1)
+            out[b * G:b * G + r, h * grp * hd:(h + 1) * grp * hd] = o
+    return out
