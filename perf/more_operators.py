@@ -710,7 +710,7 @@ def run(s):
             archer.pages_copy(s["data"], p.copy_src, p.copy_dst)
             return dict(p._asdict(), forked=table, free=s["free"], data=s["data"])
         m = archer.pages_compact(s["new"], c["page"], p.table, p.refs)
-        archer.pages_copy(s["data"], m.move_src, m.move_dst)
+        archer.pages_copy(s["data"], m.move_src, m.move_dst, count=m.moves)
         return dict(m._asdict(), data=s["data"])
     cache = archer.Cache8(s["data"], c["page"], c["hd"])
     if c["kind"] == "store":
