@@ -189,6 +189,74 @@ archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4 *cac
                                          const int32_t *resp_len, void *O, void *workspace, size_t ws_bytes,
                                          void *hip_stream);
 
+/* ---- pages that several sequences share ----------------------------------------
+ * Block tables, the ring of free pages and slots as in archer_cache4_plan, with a count
+ * refs[p] of the table rows that hold page p (device int32 [n_pages]; 0: free): samples of
+ * one prompt list its pages, and only what a sample writes is its own.  For any cache
+ * of pages (archer_cache4, archer_cache8): one call serves every layer's.  No call
+ * synchronises.  Every row holds a page at most once, and counts and tables agree with
+ * each other; of that no more is checked than keeps the calls inside their arrays.
+ * In-and-out pairs (refs_in, refs_out; table_in, table_out) may be the same array: then
+ * the call changes it in place; otherwise they must not overlap, and the call
+ * may be repeated with the same result.  Other arrays must not overlap.
+ *
+ * archer_pages_fork: row dst[i] of the table gets the pages of the first len[i] tokens of row
+ * src[i], i < n <= 4096, each page one holder more.  Rows dst held nothing before
+ * (archer_pages_plan frees a row); the rest of them stays as it is.
+ *   table   [n_rows][max_pages], n_rows <= 65536
+ *   status  [1]: 0, or 2 and nothing changed (refs_out = refs_in): a row outside the table, a
+ *           length beyond max_pages, a dst twice, or a dst that is a src */
+archer_status archer_pages_fork(int32_t n, const int32_t *src, const int32_t *dst, const int32_t *len,
+                                int32_t page_size, int32_t n_pages, int32_t n_rows, int32_t max_pages,
+                                int32_t *table, const int32_t *refs_in, int32_t *refs_out, int32_t *status,
+                                void *hip_stream);
+
+/* archer_cache4_plan for rows that share pages: rows go from len_old[b] to len_new[b] tokens
+ * (batch <= 4096), with len_new 0 to the end of their request.
+ *   - A row that shrinks drops its last pages, each one holder less.  Those without a holder
+ *     left go behind the ring's end, in the order of the last row that drops them.
+ *   - A row that grows from inside its last page (len_old no multiple of page_size) writes to
+ *     it.  While others hold that page, after this call's drops, the row takes one of its own,
+ *     and the page has to be copied to it (archer_pages_copy) before the row's new tokens are
+ *     stored.  Where all of a page's holders write, the last of them keeps it.
+ *   - Pages are taken from the ring's front in row order, a row's copy first; each has one holder.
+ *   pool_in, pool_out, row_off, slot_map, status   as in archer_cache4_plan; slots are those after
+ *             the copies.  Status 4 also where a page that is dropped or written to is none of the
+ *             pool's.  Of a status other than 0: nothing changed, copies -1.
+ *   copy_src, copy_dst [batch]: the page that row b's copy is made of and the new one, or -1
+ *   workspace  device scratch of archer_pages_plan_ws_bytes bytes (0 for a bad shape), 256-byte aligned */
+size_t archer_pages_plan_ws_bytes(int32_t batch, int32_t n_pages);
+archer_status archer_pages_plan(int32_t batch, const int32_t *len_old, const int32_t *len_new, int32_t page_size,
+                                int32_t n_pages, int32_t max_pages, const int32_t *table_in, int32_t *table_out,
+                                int32_t *free_pages, const int32_t *pool_in, int32_t *pool_out,
+                                const int32_t *refs_in, int32_t *refs_out, int32_t *row_off, int32_t *slot_map,
+                                int32_t slot_rows, int32_t *copy_src, int32_t *copy_dst, int32_t *status,
+                                void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Moves the pages in use to the front of the pool, so that its end can be given away: with U
+ * pages in use, those from U on, in rising order, move to the free ones below U, in
+ * rising order.  The tables are rewritten at once; the pages' bytes move with
+ * archer_pages_copy(move_src, move_dst, moves), before they are next read.
+ *   table     [batch][max_pages]; a row's pages are those of its first len[b] tokens (clamped
+ *             to [0, max_pages * page_size]), the other entries stay as they are
+ *   free_pages [n_pages], pool_out [2]: the new ring: pages U .. n_pages - 1, then -1; 0 and their number
+ *   move_src, move_dst [n_pages / 2]: the moves, then -1; moves [1]: their number
+ *   workspace  device scratch of archer_pages_compact_ws_bytes bytes, 256-byte aligned */
+size_t archer_pages_compact_ws_bytes(int32_t n_pages);
+archer_status archer_pages_compact(int32_t batch, const int32_t *len, int32_t page_size, int32_t n_pages,
+                                   int32_t max_pages, const int32_t *table_in, int32_t *table_out,
+                                   const int32_t *refs_in, int32_t *refs_out, int32_t *free_pages,
+                                   int32_t *pool_out, int32_t *move_src, int32_t *move_dst, int32_t *moves,
+                                   void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Copies page src[i] to page dst[i], i < n (and < *count, device int32, where count is not NULL),
+ * in each of n_planes pools (one per layer) plane_stride bytes apart, of n_pages pages of
+ * page_bytes bytes, a multiple of 16 (a cache's bytes / n_pages); data 16-byte aligned.  Pairs with
+ * an entry outside [0, n_pages) are passed over.  No page may be a dst twice, or both a src and a dst. */
+archer_status archer_pages_copy(int64_t page_bytes, int32_t n_pages, int32_t n_planes, int64_t plane_stride,
+                                void *data, int32_t n, const int32_t *src, const int32_t *dst,
+                                const int32_t *count, void *hip_stream);
+
 /* Kernel classes for timing.  The projection classes _QKV, _O, _GATEUP and
  * _DOWN are the launches of CachedForward passes (M = G per sequence); their
  * _FULL twins are the same projections in FullForward (refresh) passes

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+from collections import namedtuple
 
 import torch
 
@@ -40,6 +41,8 @@ EXPORTED = [
     "archer_set_single_term", "archer_op_attention_noalloc", "archer_op_projection_tiles",
     "archer_cache4_bytes", "archer_cache4_plan", "archer_cache4_write", "archer_cache4_read",
     "archer_op_attention_cache4_ws_bytes", "archer_op_attention_cache4",
+    "archer_pages_fork", "archer_pages_plan_ws_bytes", "archer_pages_plan", "archer_pages_compact_ws_bytes",
+    "archer_pages_compact", "archer_pages_copy",
 ]
 FORWARD_CONTROLLER, FORWARD_REFRESH, FORWARD_CACHED = 0, 1, 2
 READ_LOGITS, READ_HIDDEN, READ_RESIDUAL, READ_PROMPT_K, READ_PROMPT_V = range(5)
@@ -155,6 +158,19 @@ lib.archer_op_attention_cache4_ws_bytes.argtypes = [C.c_int32] * 8
 lib.archer_op_attention_cache4.restype = C.c_int
 lib.archer_op_attention_cache4.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, C.c_int32, C.c_int32, P, P,
                                            C.c_int32, P, C.c_int32, P, P, C.c_int32, C.c_int32, P, P, P, C.c_size_t, P]
+lib.archer_pages_fork.restype = C.c_int
+lib.archer_pages_fork.argtypes = [C.c_int32, P, P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, P, P, P, P, P]
+lib.archer_pages_plan_ws_bytes.restype = C.c_size_t
+lib.archer_pages_plan_ws_bytes.argtypes = [C.c_int32] * 2
+lib.archer_pages_plan.restype = C.c_int
+lib.archer_pages_plan.argtypes = ([C.c_int32, P, P, C.c_int32, C.c_int32, C.c_int32] + [P] * 9 +
+                                  [C.c_int32, P, P, P, P, C.c_size_t, P])
+lib.archer_pages_compact_ws_bytes.restype = C.c_size_t
+lib.archer_pages_compact_ws_bytes.argtypes = [C.c_int32]
+lib.archer_pages_compact.restype = C.c_int
+lib.archer_pages_compact.argtypes = [C.c_int32, P, C.c_int32, C.c_int32, C.c_int32] + [P] * 10 + [C.c_size_t, P]
+lib.archer_pages_copy.restype = C.c_int
+lib.archer_pages_copy.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int64, P, C.c_int32, P, P, P, P]
 lib.archer_timing_begin.restype = C.c_int
 lib.archer_timing_begin.argtypes = [P, C.c_uint32, C.c_int32]
 lib.archer_timing_end.restype = C.c_int
@@ -661,3 +677,102 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
                                           _dev(O, otype, "O", dev), ws.data_ptr() if nbytes else None, nbytes,
                                           _raw_stream(dev)))
     return O
+
+
+# -- pages that several sequences share -----------------------------------------------------------
+PagesPlan = namedtuple("PagesPlan", "table refs pool row_off slots copy_src copy_dst status")
+PagesCompact = namedtuple("PagesCompact", "table refs free pool move_src move_dst moves")
+
+
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _pair(given, like, name, dev):
+    """An output that may be its input: the given one, or a new tensor."""
+    out = torch.empty_like(like) if given is None else given
+    if out.shape != like.shape:
+        _refuse(E_SHAPE, f"{name} must have the shape of its input")
+    return out, _dev(out, torch.int32, name, dev)
+
+
+def _table(table, rows, page_size, dev):
+    if table.dim() != 2 or (rows is not None and table.shape[0] != rows):
+        _refuse(E_SHAPE, "table must be [rows][max_pages]")
+    if not 0 <= page_size <= _I32:
+        _refuse(E_SHAPE, "page_size must not be negative and fit in 32 bits")
+    return _dev(table, torch.int32, "table", dev)
+
+
+def pages_fork(src, dst, length, page_size, table, refs, refs_out=None):
+    """archer_pages_fork: rows dst [n] of table [rows][max_pages] (in place) list the pages of the first length [n]
+    tokens of rows src [n].  Returns refs [n_pages] after it (refs_out; given refs itself: in place) and status [1]."""
+    n, dev = src.numel(), torch.cuda.current_device()
+    t = _table(table, None, page_size, dev)
+    refs_out, out = _pair(refs_out, refs, "refs_out", dev)
+    status = torch.empty(1, dtype=torch.int32, device=table.device)
+    _check(lib.archer_pages_fork(n, _i32(src, n, "src", dev), _i32(dst, n, "dst", dev), _i32(length, n, "length", dev),
+                                 page_size, refs.numel(), table.shape[0], table.shape[1], t,
+                                 _dev(refs, torch.int32, "refs", dev), out, status.data_ptr(), _raw_stream(dev)))
+    return refs_out, status
+
+
+def pages_plan(len_old, len_new, page_size, table, free_pages, pool, refs, slot_rows, table_out=None, refs_out=None):
+    """archer_pages_plan: the rows of table [B][max_pages] go from len_old to len_new tokens; free_pages [n_pages]
+    changes in place.  table_out and refs_out may be table and refs (in place); new tensors by default.
+    Returns PagesPlan(table, refs, pool, row_off, slots, copy_src, copy_dst, status)."""
+    B, dev = len_old.numel(), torch.cuda.current_device()
+    t = _table(table, B, page_size, dev)
+    if not 0 <= slot_rows <= _I32:
+        _refuse(E_SHAPE, "slot_rows must not be negative and fit in 32 bits")
+    n_pages = refs.numel()
+    table_out, t_out = _pair(table_out, table, "table_out", dev)
+    refs_out, r_out = _pair(refs_out, refs, "refs_out", dev)
+    out = torch.empty(slot_rows + 3 * B + 4, dtype=torch.int32, device=len_old.device)
+    slots, off, src, dst, pool_out, status = out.split((slot_rows, B + 1, B, B, 2, 1))
+    ws = _scratch(lib.archer_pages_plan_ws_bytes(B, n_pages), len_old.device)
+    p = out.data_ptr()
+    at = [p + 4 * k for k in (slot_rows, slot_rows + B + 1, slot_rows + 2 * B + 1, slot_rows + 3 * B + 1, slot_rows + 3 * B + 3)]
+    _check(lib.archer_pages_plan(B, _i32(len_old, B, "len_old", dev), _i32(len_new, B, "len_new", dev), page_size, n_pages,
+                                 table.shape[1], t, t_out, _i32(free_pages, n_pages, "free_pages", dev),
+                                 _i32(pool, 2, "pool", dev), at[3], _dev(refs, torch.int32, "refs", dev), r_out, at[0], p,
+                                 slot_rows, at[1], at[2], at[4], ws.data_ptr(), ws.numel(), _raw_stream(dev)))
+    return PagesPlan(table_out, refs_out, pool_out, off, slots, src, dst, status)
+
+
+def pages_compact(length, page_size, table, refs, table_out=None, refs_out=None):
+    """archer_pages_compact: the pages in use move to the front of the pool; the rows of table [B][max_pages] hold
+    length [B] tokens.  table_out and refs_out may be table and refs (in place); new tensors by default.
+    Returns PagesCompact(table, refs, free, pool, move_src, move_dst, moves); pages_copy moves the bytes."""
+    B, dev, n_pages = length.numel(), torch.cuda.current_device(), refs.numel()
+    t = _table(table, B, page_size, dev)
+    table_out, t_out = _pair(table_out, table, "table_out", dev)
+    refs_out, r_out = _pair(refs_out, refs, "refs_out", dev)
+    half = n_pages // 2
+    out = torch.empty(n_pages + 2 * half + 3, dtype=torch.int32, device=length.device)
+    free, src, dst, pool, moves = out.split((n_pages, half, half, 2, 1))
+    ws = _scratch(lib.archer_pages_compact_ws_bytes(n_pages), length.device)
+    p = out.data_ptr()
+    _check(lib.archer_pages_compact(B, _i32(length, B, "length", dev), page_size, n_pages, table.shape[1], t, t_out,
+                                    _dev(refs, torch.int32, "refs", dev), r_out, p, p + 4 * (n_pages + 2 * half),
+                                    p + 4 * n_pages, p + 4 * (n_pages + half), p + 4 * (n_pages + 2 * half + 2),
+                                    ws.data_ptr(), ws.numel(), _raw_stream(dev)))
+    return PagesCompact(table_out, refs_out, free, pool, src, dst, moves)
+
+
+def pages_copy(data, src, dst, count=None):
+    """archer_pages_copy: page src[i] of data ([n_pages][heads][bytes], a cache's, or [planes][n_pages][heads][bytes], every
+    layer's) to page dst[i], i < src.numel() and < count [1] (device), where it is given.  Entries of -1 are passed over."""
+    n, dev = src.numel(), torch.cuda.current_device()
+    if data.dim() not in (3, 4):
+        _refuse(E_SHAPE, "data must be [n_pages][heads][bytes] or [planes][n_pages][heads][bytes]")
+    planes = data.shape[0] if data.dim() == 4 else 1
+    n_pages, heads, width = data.shape[-3:]
+    if planes < 1 or n_pages < 1:
+        _refuse(E_SHAPE, "data must hold a page")
+    if planes > _I32 or n_pages > _I32 or n > _I32:
+        _refuse(E_SHAPE, "planes, pages and pairs must fit in 32 bits")
+    page = heads * width * data.element_size()
+    _check(lib.archer_pages_copy(page, n_pages, planes, page * n_pages, _dev(data, data.dtype, "data", dev), n,
+                                 _i32(src, n, "src", dev), _i32(dst, n, "dst", dev),
+                                 None if count is None else _i32(count, 1, "count", dev), _raw_stream(dev)))

@@ -7,6 +7,7 @@
 #include "archer_ops.h"
 #include "cache4.h"
 #include "errors.h"
+#include "host_checks.h"
 
 namespace {
 
@@ -15,21 +16,6 @@ namespace {
     hipError_t e_ = (x);                                                                                       \
     if (e_ != hipSuccess) return archer_fail(ARCHER_E_HIP, std::string(#x) + ": " + hipGetErrorString(e_));    \
   } while (0)
-
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-// log2 of a page size, or -1
-int page_shift(int32_t page_size) {
-  for (int s = 5; s <= 8; ++s)
-    if (page_size == 1 << s) return s;
-  return -1;
-}
-
-const char* pages_error(int32_t page_size, int32_t n_pages) {
-  if (page_shift(page_size) < 0) return "page_size must be 32, 64, 128 or 256";
-  if (n_pages < 1 || (long long)n_pages * page_size > INT_MAX) return "n_pages must be positive, n_pages * page_size below 2^31";
-  return nullptr;
-}
 
 // Shape checks of a cache; data may still be null
 const char* cache_error(const archer_cache4* c) {
