@@ -189,6 +189,64 @@ archer_status archer_op_attention_cache4(int32_t dtype, const archer_cache4 *cac
                                          const int32_t *resp_len, void *O, void *workspace, size_t ws_bytes,
                                          void *hip_stream);
 
+/* ---- 8-bit paged prompt cache -------------------------------------------------
+ * One layer's keys and values in e4m3 (sign, four exponent bits, three mantissa bits, at
+ * most 448) with one power-of-two scale per block of 32 tokens and head, for its keys and for its
+ * values: 256 bytes per token and head of 128 dimensions, and 16 a page.  Pages, slots and
+ * block tables as for the 4-bit cache: plans are archer_cache4_plan's or, for pages that
+ * sequences share, archer_pages_plan's.
+ *
+ * data: device, 16-byte aligned, archer_cache8_bytes bytes, caller-owned.
+ * [n_pages][n_kv_heads] blocks of page_size * 2 * head_dim + 16 bytes:
+ *   keys    [page_size][head_dim]
+ *   values  [page_size / 8][head_dim / 32][16][2][8]   dimension u head_dim / 16 + 2 i + s of
+ *           token t of an 8-token block is at [i][u][s][t]
+ *   scales  [page_size / 32][2]   exponent + 127 of a block's keys, of its values; then unused
+ * page_size 32, 64, 128 or 256; head_dim 64 or 128; n_pages * page_size < 2^31. */
+typedef struct {
+  void *data;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+} archer_cache8;
+
+/* Bytes of the cache's data (0 and last_error for a bad shape; data is not read). */
+size_t archer_cache8_bytes(const archer_cache8 *cache);
+
+/* Store rows of keys and values (fp16 for ARCHER_BF16, fp32 for ARCHER_FP32): rows row_off[b] ..
+ * row_off[b + 1] - 1 become the tokens from position start[b] on of sequence b, b < batch, whose
+ * pages row b of the block table lists.  A sequence ends with the last row stored: of later tokens
+ * in that row's block nothing is kept.
+ *   table    device int32 [batch][max_pages]; tokens of an entry outside [0, n_pages), or beyond
+ *            the row of the table, are not stored.  A page that is stored to is one sequence's.
+ *   start    device int32 [batch], >= 0
+ *   row_off  device int32 [batch + 1], rising; rows beyond `rows` (host; sizes the launch) are not stored
+ * Element (head, row, d) is at K[head k_head + row k_row + d] and V[head v_head + row v_row + d
+ * v_dim] (strides in elements, any sign), with v_dim = 1 or v_row = 1 (else ARCHER_E_UNSUPPORTED; of a
+ * single row any v_dim will do).
+ * A block's scale is 2^e, e the least integer with max |x| <= 448 * 2^e over its new rows, clamped
+ * to [-15, 7]; elements are rounded to the nearest e4m3 value of x / 2^e, ties to the even code, and
+ * saturate at 448 * 2^e (57344 at most).  Where a block holds earlier tokens of the sequence e
+ * is no less than theirs, and they are rounded once more in the new scale (exact but for elements
+ * below 2^-14 of the block's largest).  Every stored element is exact in fp16.  A NaN stays one. */
+archer_status archer_cache8_write(int32_t dtype, const archer_cache8 *cache, int32_t batch, const int32_t *table,
+                                  int32_t max_pages, const int32_t *start, const int32_t *row_off, int32_t rows,
+                                  const void *K, int64_t k_head, int64_t k_row, const void *V, int64_t v_head,
+                                  int64_t v_row, int64_t v_dim, void *hip_stream);
+
+/* The stored elements of the slots slot_map[row], as archer_cache4_read. */
+archer_status archer_cache8_read(int32_t dtype, const archer_cache8 *cache, int32_t rows,
+                                 const int32_t *slot_map, void *K, void *V, void *hip_stream);
+
+/* archer_op_attention_cache4 over the 8-bit cache: the same arguments, limits and results of rows
+ * without keys.  fp16: probabilities are rounded to fp16, and nothing else is but the output. */
+size_t archer_op_attention_cache8_ws_bytes(int32_t dtype, int32_t batch, int32_t G, int32_t Hq, int32_t Hkv,
+                                           int32_t hd, int32_t max_cached, int32_t fresh);
+archer_status archer_op_attention_cache8(int32_t dtype, const archer_cache8 *cache, int32_t batch, int32_t G,
+                                         int32_t Hq, const void *Q, const int32_t *table, int32_t max_pages,
+                                         const int32_t *cached_len, int32_t max_cached, const void *K2,
+                                         const void *Vt2, int32_t ld2, int32_t fresh_stride,
+                                         const int32_t *resp_len, void *O, void *workspace, size_t ws_bytes,
+                                         void *hip_stream);
+
 /* ---- pages that several sequences share ----------------------------------------
  * Block tables, the ring of free pages and slots as in archer_cache4_plan, with a count
  * refs[p] of the table rows that hold page p (device int32 [n_pages]; 0: free): samples of

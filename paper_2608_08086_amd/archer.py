@@ -43,6 +43,8 @@ EXPORTED = [
     "archer_op_attention_cache4_ws_bytes", "archer_op_attention_cache4",
     "archer_pages_fork", "archer_pages_plan_ws_bytes", "archer_pages_plan", "archer_pages_compact_ws_bytes",
     "archer_pages_compact", "archer_pages_copy",
+    "archer_cache8_bytes", "archer_cache8_write", "archer_cache8_read",
+    "archer_op_attention_cache8_ws_bytes", "archer_op_attention_cache8",
 ]
 FORWARD_CONTROLLER, FORWARD_REFRESH, FORWARD_CACHED = 0, 1, 2
 READ_LOGITS, READ_HIDDEN, READ_RESIDUAL, READ_PROMPT_K, READ_PROMPT_V = range(5)
@@ -91,6 +93,8 @@ class Cache4Desc(C.Structure):
     _fields_ = [("data", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32)]
 
+
+Cache8Desc = Cache4Desc      # archer_cache8 has the same fields
 
 P = C.c_void_p
 lib.archer_workspace_bytes.restype = C.c_size_t
@@ -158,6 +162,17 @@ lib.archer_op_attention_cache4_ws_bytes.argtypes = [C.c_int32] * 8
 lib.archer_op_attention_cache4.restype = C.c_int
 lib.archer_op_attention_cache4.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, C.c_int32, C.c_int32, P, P,
                                            C.c_int32, P, C.c_int32, P, P, C.c_int32, C.c_int32, P, P, P, C.c_size_t, P]
+lib.archer_cache8_bytes.restype = C.c_size_t
+lib.archer_cache8_bytes.argtypes = [C.POINTER(Cache4Desc)]
+lib.archer_cache8_write.restype = C.c_int
+lib.archer_cache8_write.argtypes = [C.c_int32, C.POINTER(Cache4Desc), C.c_int32, P, C.c_int32, P, P, C.c_int32, P, C.c_int64,
+                                    C.c_int64, P, C.c_int64, C.c_int64, C.c_int64, P]
+lib.archer_cache8_read.restype = C.c_int
+lib.archer_cache8_read.argtypes = lib.archer_cache4_read.argtypes
+lib.archer_op_attention_cache8_ws_bytes.restype = C.c_size_t
+lib.archer_op_attention_cache8_ws_bytes.argtypes = [C.c_int32] * 8
+lib.archer_op_attention_cache8.restype = C.c_int
+lib.archer_op_attention_cache8.argtypes = lib.archer_op_attention_cache4.argtypes
 lib.archer_pages_fork.restype = C.c_int
 lib.archer_pages_fork.argtypes = [C.c_int32, P, P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, P, P, P, P, P]
 lib.archer_pages_plan_ws_bytes.restype = C.c_size_t
@@ -552,9 +567,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-class Cache4:
-    """One layer's 4-bit paged cache (archer_cache4): data uint8 [n_pages][n_kv_heads][page bytes]."""
-
+class _PagedCache:
     def __init__(self, data, page_size, head_dim):
         if data.dim() != 3:
             _refuse(E_SHAPE, "data must be [n_pages][n_kv_heads][page bytes]")
@@ -566,11 +579,11 @@ class Cache4:
         self.desc = Cache4Desc(_dev(data, torch.uint8, "data", torch.cuda.current_device()), self.n_pages, page_size,
                                self.n_kv_heads, head_dim)
         self.ref = C.byref(self.desc)
-        n = lib.archer_cache4_bytes(self.ref)
+        n = self._bytes(self.ref)
         if n == 0:
             _refuse(E_SHAPE, lib.archer_last_error().decode())
         if n != data.numel():
-            _refuse(E_SHAPE, f"a page of {page_size} tokens has {page_size * (head_dim + head_dim // 16)} bytes "
+            _refuse(E_SHAPE, f"a page of {page_size} tokens has {self.page_bytes(page_size, head_dim)} bytes "
                              f"per head, not {page_bytes}")
 
     @property
@@ -580,8 +593,26 @@ class Cache4:
 
     @classmethod
     def empty(cls, n_pages, page_size, n_kv_heads, head_dim):
-        return cls(torch.zeros(n_pages, n_kv_heads, page_size * (head_dim + head_dim // 16), dtype=torch.uint8,
+        return cls(torch.zeros(n_pages, n_kv_heads, cls.page_bytes(page_size, head_dim), dtype=torch.uint8,
                                device="cuda"), page_size, head_dim)
+
+
+class Cache4(_PagedCache):
+    """One layer's 4-bit paged cache (archer_cache4): data uint8 [n_pages][n_kv_heads][page bytes]."""
+    _bytes = lib.archer_cache4_bytes
+
+    @staticmethod
+    def page_bytes(page_size, head_dim):
+        return page_size * (head_dim + head_dim // 16)
+
+
+class Cache8(_PagedCache):
+    """One layer's 8-bit paged cache (archer_cache8): data uint8 [n_pages][n_kv_heads][page bytes]."""
+    _bytes = lib.archer_cache8_bytes
+
+    @staticmethod
+    def page_bytes(page_size, head_dim):
+        return page_size * 2 * head_dim + 16
 
 
 def cache4_plan(len_old, len_new, page_size, table, free_pages, pool, slot_rows):
@@ -604,7 +635,7 @@ def cache4_plan(len_old, len_new, page_size, table, free_pages, pool, slot_rows)
     return pool_out, row_off, slot_map, status
 
 
-def _cache4_dtype(t, name):
+def _cache_dtype(t, name):
     if t == torch.float16:
         return BF16
     if t != torch.float32:
@@ -615,7 +646,8 @@ def _cache4_dtype(t, name):
 def cache4_write(cache, K, V, slot_map):
     """archer_cache4_write: K, V [n_kv_heads][rows][head_dim] (views; K with unit stride along the last
     dimension, V along the last or the row dimension) into the slots slot_map [rows]."""
-    dt, dev = _cache4_dtype(K.dtype, "K"), torch.cuda.current_device()
+    _of(cache, Cache4)
+    dt, dev = _cache_dtype(K.dtype, "K"), torch.cuda.current_device()
     rows = slot_map.numel()
     shape = (cache.n_kv_heads, rows, cache.head_dim)
     if K.shape != shape or V.shape != shape:
@@ -629,22 +661,38 @@ def cache4_write(cache, K, V, slot_map):
                                    _raw_stream(dev)))
 
 
-def cache4_read(cache, slot_map, dtype=torch.float16):
-    """archer_cache4_read: the stored rows of slot_map, K and V [n_kv_heads][rows][head_dim]."""
-    dt, dev = _cache4_dtype(dtype, "dtype"), torch.cuda.current_device()
+def _of(cache, kind):
+    """The other format's pages have other sizes: their bytes would be taken for something else."""
+    if not isinstance(cache, kind):
+        _refuse(E_ARG, f"the cache must be a {kind.__name__}")
+
+
+def _read(call, cache, slot_map, dtype):
+    dt, dev = _cache_dtype(dtype, "dtype"), torch.cuda.current_device()
     rows = slot_map.numel()
     _dev(cache.data, torch.uint8, "the cache", dev)
     K, V = torch.empty(2, cache.n_kv_heads, rows, cache.head_dim, dtype=dtype, device=cache.data.device).unbind()
-    _check(lib.archer_cache4_read(dt, cache.ref, rows, _i32(slot_map, rows, "slot_map", dev), K.data_ptr(), V.data_ptr(),
-                                  _raw_stream(dev)))
+    _check(call(dt, cache.ref, rows, _i32(slot_map, rows, "slot_map", dev), K.data_ptr(), V.data_ptr(), _raw_stream(dev)))
     return K, V
+
+
+def cache4_read(cache, slot_map, dtype=torch.float16):
+    """archer_cache4_read: the stored rows of slot_map, K and V [n_kv_heads][rows][head_dim]."""
+    _of(cache, Cache4)
+    return _read(lib.archer_cache4_read, cache, slot_map, dtype)
 
 
 def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=None, fresh_stride=0, resp_len=None, O=None):
     """archer_op_attention_cache4: Q [Hq][B G][hd] (fp16: O bf16; fp32: O fp32), table [B][max_pages], cached_len [B],
     optional fresh K2 [Hkv][ld2][hd] and Vt2 [Hkv][hd][ld2], optional resp_len [B].  Returns O [B G][Hq hd]
     (preallocated if given: rows past resp_len are not written)."""
-    dt, dev = _cache4_dtype(Q.dtype, "Q"), torch.cuda.current_device()
+    _of(cache, Cache4)
+    return _attention(lib.archer_op_attention_cache4_ws_bytes, lib.archer_op_attention_cache4, Q, cache, table, cached_len,
+                      max_cached, K2, Vt2, fresh_stride, resp_len, O)
+
+
+def _attention(ws_bytes, call, Q, cache, table, cached_len, max_cached, K2, Vt2, fresh_stride, resp_len, O):
+    dt, dev = _cache_dtype(Q.dtype, "Q"), torch.cuda.current_device()
     _dev(cache.data, torch.uint8, "the cache", dev)
     if Q.dim() != 3 or table.dim() != 2:
         _refuse(E_SHAPE, "Q must be [Hq][B G][hd], table [B][max_pages]")
@@ -668,15 +716,49 @@ def op_attention_cache4(Q, cache, table, cached_len, max_cached, K2=None, Vt2=No
         O = torch.empty(rows, Hq * hd, dtype=otype, device=Q.device)
     elif O.shape != (rows, Hq * hd):
         _refuse(E_SHAPE, "O must be [B G][Hq hd]")
-    nbytes = lib.archer_op_attention_cache4_ws_bytes(dt, B, G, Hq, Hkv, hd, max_cached, int(k2 is not None))
+    nbytes = ws_bytes(dt, B, G, Hq, Hkv, hd, max_cached, int(k2 is not None))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
-    _check(lib.archer_op_attention_cache4(dt, cache.ref, B, G, Hq, _dev(Q, Q.dtype, "Q", dev),
-                                          _i32(table, B * width, "table", dev), width,
-                                          _i32(cached_len, B, "cached_len", dev), max_cached, k2, v2, ld2, fresh_stride,
-                                          None if resp_len is None else _i32(resp_len, B, "resp_len", dev),
-                                          _dev(O, otype, "O", dev), ws.data_ptr() if nbytes else None, nbytes,
-                                          _raw_stream(dev)))
+    _check(call(dt, cache.ref, B, G, Hq, _dev(Q, Q.dtype, "Q", dev), _i32(table, B * width, "table", dev), width,
+                _i32(cached_len, B, "cached_len", dev), max_cached, k2, v2, ld2, fresh_stride,
+                None if resp_len is None else _i32(resp_len, B, "resp_len", dev), _dev(O, otype, "O", dev),
+                ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)))
     return O
+
+
+# -- the 8-bit paged prompt cache -----------------------------------------------------------------
+def cache8_write(cache, table, start, row_off, K, V):
+    """archer_cache8_write: K, V [n_kv_heads][rows][head_dim] (views; K with unit stride along the last dimension, V
+    along the last or the row dimension): rows row_off[b] .. row_off[b + 1] - 1 (row_off [B + 1]) become the tokens from
+    position start[b] on of the sequence of row b of table [B][max_pages].  Rows from row_off[B] on are not stored."""
+    _of(cache, Cache8)
+    dt, dev = _cache_dtype(K.dtype, "K"), torch.cuda.current_device()
+    if table.dim() != 2 or K.dim() != 3:
+        _refuse(E_SHAPE, "table must be [B][max_pages], K and V [n_kv_heads][rows][head_dim]")
+    (B, width), rows = table.shape, K.shape[1]
+    shape = (cache.n_kv_heads, rows, cache.head_dim)
+    if K.shape != shape or V.shape != shape:
+        _refuse(E_SHAPE, f"K and V must be {list(shape)}")
+    (kh, kr, kd), (vh, vr, vd) = K.stride(), V.stride()
+    if kd != 1:
+        _refuse(E_UNSUPPORTED, "K must have unit stride along its dimensions")
+    _dev(cache.data, torch.uint8, "the cache", dev)
+    _check(lib.archer_cache8_write(dt, cache.ref, B, _dev(table, torch.int32, "table", dev), width,
+                                   _i32(start, B, "start", dev), _i32(row_off, B + 1, "row_off", dev), rows,
+                                   _dev(K, K.dtype, "K", dev, True), kh, kr, _dev(V, K.dtype, "V", dev, True), vh, vr, vd,
+                                   _raw_stream(dev)))
+
+
+def cache8_read(cache, slot_map, dtype=torch.float16):
+    """archer_cache8_read: the stored rows of slot_map, K and V [n_kv_heads][rows][head_dim]."""
+    _of(cache, Cache8)
+    return _read(lib.archer_cache8_read, cache, slot_map, dtype)
+
+
+def op_attention_cache8(Q, cache, table, cached_len, max_cached, K2=None, Vt2=None, fresh_stride=0, resp_len=None, O=None):
+    """archer_op_attention_cache8: as op_attention_cache4, over a Cache8."""
+    _of(cache, Cache8)
+    return _attention(lib.archer_op_attention_cache8_ws_bytes, lib.archer_op_attention_cache8, Q, cache, table, cached_len,
+                      max_cached, K2, Vt2, fresh_stride, resp_len, O)
 
 
 # -- pages that several sequences share -----------------------------------------------------------

@@ -18,10 +18,7 @@
 // tokens share a byte, so tokens are stored without read-modify-write.
 #pragma once
 
-#include "common.h"
-
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+#include "paged.h"
 
 constexpr int C4_EMIN = 104, C4_EMAX = 140;   // biased scale exponents: 2^-23 .. 2^13
 constexpr int C4_NAN = 255;                   // scale byte of a block that holds a NaN
@@ -38,11 +35,6 @@ template <int HD> struct C4 {
   __device__ static int vsoff(int T) { return T * HD + T * (HD / 32); }
 };
 
-struct C4Pool {
-  uint8_t* data;
-  int n_pages, psh, hkv;     // page size 1 << psh
-};
-
 struct C4PlanArgs {
   const int *len_old, *len_new;
   int batch, psh, n_pages, width;   // width: entries of a table row
@@ -53,7 +45,7 @@ struct C4PlanArgs {
 };
 
 struct C4RowsArgs {
-  C4Pool c;
+  PagePool c;
   const void *K, *V;            // write: sources (strides in elements); read: unused
   long k_head, k_row, v_head, v_row, v_dim;
   void *Ko, *Vo;                // read: [hkv][rows][hd]
@@ -61,32 +53,8 @@ struct C4RowsArgs {
   int rows;
 };
 
-struct Attn4Args {
-  C4Pool c;
-  const void* Q;                // [hq][batch * G][hd]
-  const int* table;
-  int width;
-  const int* cached_len;
-  int max_cached;
-  const void *K2, *Vt2;         // fresh segment, or null: [hkv][ld2][hd], [hkv][hd][ld2]
-  int ld2, fstride;
-  const int* resp_len;          // or null
-  void* O;                      // [batch * G][hq * hd]
-  float *Opart, *ML;            // chunk partials [slots][hkv][G * hq / hkv][hd], and (m, l) of each
-  int batch, G, hq, hkv, hd;
-  int target, chunk_min, slots, step; // see Attn4Split
-  int sorted;                   // row kernel: sequences in the order of falling length
-  float scale_log2;
-};
-
-// How a call's keys are cut, from what the host knows of it: chunks of
-// max(all steps / target, chunk_min) steps, at most `slots` of them (target 0: one per sequence).
-struct Attn4Split {
-  int target, chunk_min, slots, step;   // step: keys of a step
-};
-
 void launch_cache4_plan(const C4PlanArgs& a, hipStream_t st);
 int launch_cache4_write(int fp32, int hd, const C4RowsArgs& a, hipStream_t st);
 int launch_cache4_read(int fp32, int hd, const C4RowsArgs& a, hipStream_t st);
-Attn4Split attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh);
-int launch_attn4(int fp32, const Attn4Args& a, hipStream_t st);
+AttnSplit attn4_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh);
+void launch_attn4(int fp32, const PagedAttnArgs& a, hipStream_t st);
