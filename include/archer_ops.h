@@ -315,6 +315,33 @@ archer_status archer_pages_copy(int64_t page_bytes, int32_t n_pages, int32_t n_p
                                 void *data, int32_t n, const int32_t *src, const int32_t *dst,
                                 const int32_t *count, void *hip_stream);
 
+/* ---- sampling --------------------------------------------------------------------
+ * A token for each row of logits, from given random numbers: what archer_decide's unmasking
+ * takes greedily (xhat, and its log-probability) drawn instead.
+ *   logits  [rows][vocab] of type dtype (ARCHER_FP32, as a forward gives them, ARCHER_BF16 or
+ *           ARCHER_FP16), rows row_stride elements apart (any); vocab <= 524288
+ *   exclude a token that is never drawn (MASK), or -1
+ *   u       device float [rows], in [0, 1)
+ *   temperature, top_k, top_p, min_p   device float, int32, float, float [rows], or NULL: 1, and off
+ *   token   device int32 [rows]
+ *   logp    device float [rows], or NULL: log-probability of the token in what it was drawn from
+ * With z = logit / temperature, w = exp(z - max z) and the tokens ordered by falling logit, equal
+ * ones by rising index:
+ *   S1  the first top_k tokens (top_k < 1: all)
+ *   S2  the shortest prefix of S1 whose weight is at least top_p of S1's (top_p >= 1: S1; <= 0: one token)
+ *   S3  the tokens with w >= min_p (min_p <= 0: all)
+ * kept are the tokens of S2 that are in S3, and the first token of the order always; the token
+ * drawn is the first one by index at which the sum of the kept weights up to it exceeds u times all of
+ * it (with rounding at u near 1: the last one of any weight).  A temperature that is not
+ * positive takes the first token of the order, with logp 0.  Weights are summed in 64 bits, by fixed
+ * orders: a row's result does not depend on the other rows or on the run.  Infinite logits share
+ * the weight; -infinity has none.  A row without a token (all -infinity or excluded): token -1, logp
+ * -infinity; a row with a NaN: token -1, logp NaN. */
+archer_status archer_op_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t row_stride,
+                               int32_t exclude, const float *u, const float *temperature, const int32_t *top_k,
+                               const float *top_p, const float *min_p, int32_t *token, float *logp,
+                               void *hip_stream);
+
 /* Kernel classes for timing.  The projection classes _QKV, _O, _GATEUP and
  * _DOWN are the launches of CachedForward passes (M = G per sequence); their
  * _FULL twins are the same projections in FullForward (refresh) passes

@@ -44,7 +44,7 @@ EXPORTED = [
     "archer_pages_fork", "archer_pages_plan_ws_bytes", "archer_pages_plan", "archer_pages_compact_ws_bytes",
     "archer_pages_compact", "archer_pages_copy",
     "archer_cache8_bytes", "archer_cache8_write", "archer_cache8_read",
-    "archer_op_attention_cache8_ws_bytes", "archer_op_attention_cache8",
+    "archer_op_attention_cache8_ws_bytes", "archer_op_attention_cache8", "archer_op_sample",
 ]
 FORWARD_CONTROLLER, FORWARD_REFRESH, FORWARD_CACHED = 0, 1, 2
 READ_LOGITS, READ_HIDDEN, READ_RESIDUAL, READ_PROMPT_K, READ_PROMPT_V = range(5)
@@ -186,6 +186,8 @@ lib.archer_pages_compact.restype = C.c_int
 lib.archer_pages_compact.argtypes = [C.c_int32, P, C.c_int32, C.c_int32, C.c_int32] + [P] * 10 + [C.c_size_t, P]
 lib.archer_pages_copy.restype = C.c_int
 lib.archer_pages_copy.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int64, P, C.c_int32, P, P, P, P]
+lib.archer_op_sample.restype = C.c_int
+lib.archer_op_sample.argtypes = [C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, C.c_int32] + [P] * 8
 lib.archer_timing_begin.restype = C.c_int
 lib.archer_timing_begin.argtypes = [P, C.c_uint32, C.c_int32]
 lib.archer_timing_end.restype = C.c_int
@@ -858,3 +860,38 @@ def pages_copy(data, src, dst, count=None):
     _check(lib.archer_pages_copy(page, n_pages, planes, page * n_pages, _dev(data, data.dtype, "data", dev), n,
                                  _i32(src, n, "src", dev), _i32(dst, n, "dst", dev),
                                  None if count is None else _i32(count, 1, "count", dev), _raw_stream(dev)))
+
+
+# -- sampling ---------------------------------------------------------------------------------------
+_LOGIT_DTYPES = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
+
+
+def op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, exclude=-1):
+    """archer_op_sample: logits [rows][vocab] (fp32, bf16 or fp16; a view with unit stride along the vocabulary), u [rows] in
+    [0, 1); temperature, top_p and min_p [rows] fp32, top_k [rows] int32, or None.  Returns token [rows] int32 and
+    logp [rows] fp32, the log-probability of each in what it was drawn from."""
+    dev = torch.cuda.current_device()
+    if logits.dim() != 2:
+        _refuse(E_SHAPE, "logits must be [rows][vocab]")
+    dt = _LOGIT_DTYPES.get(logits.dtype)
+    if dt is None:
+        _refuse(E_ARG, "logits must be torch.float32, torch.bfloat16 or torch.float16")
+    rows, vocab = logits.shape
+    if vocab > 1 and logits.stride(1) != 1:
+        _refuse(E_UNSUPPORTED, "logits must have unit stride along the vocabulary")
+    if not (rows <= _I32 and vocab <= _I32 and -_I32 <= exclude <= _I32):
+        _refuse(E_SHAPE, "rows, vocab and exclude must fit in 32 bits")
+
+    def per_row(t, dtype, name):
+        if t is None:
+            return None
+        if t.numel() != rows:
+            _refuse(E_SHAPE, f"{name} must have {rows} elements")
+        return _dev(t, dtype, name, dev)
+    out = torch.empty(2, rows, dtype=torch.int32, device=logits.device)
+    token, logp = out[0], out[1].view(torch.float32)
+    _check(lib.archer_op_sample(dt, rows, vocab, _dev(logits, logits.dtype, "logits", dev, True), logits.stride(0), exclude,
+                                per_row(u, torch.float32, "u"), per_row(temperature, torch.float32, "temperature"),
+                                per_row(top_k, torch.int32, "top_k"), per_row(top_p, torch.float32, "top_p"),
+                                per_row(min_p, torch.float32, "min_p"), token.data_ptr(), logp.data_ptr(), _raw_stream(dev)))
+    return token, logp
