@@ -336,11 +336,14 @@ archer_status archer_pages_copy(int64_t page_bytes, int32_t n_pages, int32_t n_p
  * positive takes the first token of the order, with logp 0.  Weights are summed in 64 bits, by fixed
  * orders: a row's result does not depend on the other rows or on the run.  Infinite logits share
  * the weight; -infinity has none.  A row without a token (all -infinity or excluded): token -1, logp
- * -infinity; a row with a NaN: token -1, logp NaN. */
+ * -infinity; a row with a NaN: token -1, logp NaN.
+ *   workspace  device scratch of archer_op_sample_ws_bytes bytes (0 for a bad shape), 256-byte aligned;
+ *              nothing in it is kept for another call */
+size_t archer_op_sample_ws_bytes(int32_t dtype, int32_t rows, int32_t vocab);
 archer_status archer_op_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t row_stride,
                                int32_t exclude, const float *u, const float *temperature, const int32_t *top_k,
                                const float *top_p, const float *min_p, int32_t *token, float *logp,
-                               void *hip_stream);
+                               void *workspace, size_t ws_bytes, void *hip_stream);
 
 /* Kernel classes for timing.  The projection classes _QKV, _O, _GATEUP and
  * _DOWN are the launches of CachedForward passes (M = G per sequence); their

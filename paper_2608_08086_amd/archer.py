@@ -44,7 +44,8 @@ EXPORTED = [
     "archer_pages_fork", "archer_pages_plan_ws_bytes", "archer_pages_plan", "archer_pages_compact_ws_bytes",
     "archer_pages_compact", "archer_pages_copy",
     "archer_cache8_bytes", "archer_cache8_write", "archer_cache8_read",
-    "archer_op_attention_cache8_ws_bytes", "archer_op_attention_cache8", "archer_op_sample",
+    "archer_op_attention_cache8_ws_bytes", "archer_op_attention_cache8",
+    "archer_op_sample_ws_bytes", "archer_op_sample",
 ]
 FORWARD_CONTROLLER, FORWARD_REFRESH, FORWARD_CACHED = 0, 1, 2
 READ_LOGITS, READ_HIDDEN, READ_RESIDUAL, READ_PROMPT_K, READ_PROMPT_V = range(5)
@@ -187,7 +188,9 @@ lib.archer_pages_compact.argtypes = [C.c_int32, P, C.c_int32, C.c_int32, C.c_int
 lib.archer_pages_copy.restype = C.c_int
 lib.archer_pages_copy.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int64, P, C.c_int32, P, P, P, P]
 lib.archer_op_sample.restype = C.c_int
-lib.archer_op_sample.argtypes = [C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, C.c_int32] + [P] * 8
+lib.archer_op_sample.argtypes = [C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, C.c_int32] + [P] * 8 + [C.c_size_t, P]
+lib.archer_op_sample_ws_bytes.restype = C.c_size_t
+lib.archer_op_sample_ws_bytes.argtypes = [C.c_int32] * 3
 lib.archer_timing_begin.restype = C.c_int
 lib.archer_timing_begin.argtypes = [P, C.c_uint32, C.c_int32]
 lib.archer_timing_end.restype = C.c_int
@@ -890,8 +893,10 @@ def op_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, e
         return _dev(t, dtype, name, dev)
     out = torch.empty(2, rows, dtype=torch.int32, device=logits.device)
     token, logp = out[0], out[1].view(torch.float32)
+    ws = _scratch(lib.archer_op_sample_ws_bytes(dt, rows, vocab), logits.device)
     _check(lib.archer_op_sample(dt, rows, vocab, _dev(logits, logits.dtype, "logits", dev, True), logits.stride(0), exclude,
                                 per_row(u, torch.float32, "u"), per_row(temperature, torch.float32, "temperature"),
                                 per_row(top_k, torch.int32, "top_k"), per_row(top_p, torch.float32, "top_p"),
-                                per_row(min_p, torch.float32, "min_p"), token.data_ptr(), logp.data_ptr(), _raw_stream(dev)))
+                                per_row(min_p, torch.float32, "min_p"), token.data_ptr(), logp.data_ptr(), ws.data_ptr(), ws.numel(),
+                                _raw_stream(dev)))
     return token, logp

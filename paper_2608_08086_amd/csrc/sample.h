@@ -17,4 +17,5 @@ struct SampleArgs {
   float* logp;                  // or null
 };
 
-void launch_sample(int dtype, const SampleArgs& a, hipStream_t st);
+size_t sample_ws_bytes(int rows);
+void launch_sample(int dtype, const SampleArgs& a, void* workspace, hipStream_t st);

@@ -63,10 +63,12 @@ X = 1 << 20
     (dict(dtype=3), "E_ARG"), (dict(dtype=-1), "E_ARG"), (dict(rows=-1), "E_SHAPE"), (dict(vocab=0), "E_SHAPE"),
     (dict(vocab=524289), "E_SHAPE"), (dict(exclude=-2), "E_ARG"), (dict(exclude=100), "E_ARG"), (dict(logits=None), "E_ARG"),
     (dict(u=None), "E_ARG"), (dict(token=None), "E_ARG"), (dict(logits=X + 2), "E_ARG"), (dict(dtype=0, logits=X + 1), "E_ARG"),
+    (dict(ws=None), "E_WORKSPACE"), (dict(ws=X + 128), "E_WORKSPACE"), (dict(ws_bytes=1000), "E_WORKSPACE"),
 ])
 def test_arguments(change, code):
     from paper_2608_08086_amd import archer as a
-    v = dict(dtype=a.FP32, rows=2, vocab=100, logits=X, stride=100, exclude=-1, u=X, t=None, k=None, p=None, m=None, token=X, logp=None)
+    v = dict(dtype=a.FP32, rows=2, vocab=100, logits=X, stride=100, exclude=-1, u=X, t=None, k=None, p=None, m=None, token=X, logp=None, ws=X,
+             ws_bytes=a.lib.archer_op_sample_ws_bytes(a.FP32, 2, 100))
     v.update(change)
     assert a.lib.archer_op_sample(*v.values(), None) == getattr(a, code)
     assert a.lib.archer_last_error()
@@ -74,7 +76,15 @@ def test_arguments(change, code):
 
 def test_no_rows():
     from paper_2608_08086_amd import archer as a
-    assert a.lib.archer_op_sample(a.FP32, 0, 100, None, 100, -1, None, None, None, None, None, None, None, None) == a.OK
+    assert a.lib.archer_op_sample(a.FP32, 0, 100, None, 100, -1, *[None] * 8, 0, None) == a.OK
+
+
+def test_workspace():
+    from paper_2608_08086_amd import archer as a
+    ws = a.lib.archer_op_sample_ws_bytes
+    assert ws(a.FP32, 1, 1) > 0 and ws(a.FP32, 1, 1) % 256 == 0
+    assert ws(3, 1, 1) == ws(a.FP32, 0, 1) == ws(a.FP32, 1, 0) == ws(a.FP32, 1, 524289) == 0
+    assert ws(a.BF16, 2**31 - 1, 152064) == ws(a.BF16, 1024, 152064) < 2**29      # many rows: in groups
 
 
 def test_binding_refusals(monkeypatch):
