@@ -23,10 +23,10 @@
 // more than 95 nats above m0, or a list too long (one value tens of thousands of times).
 //
 // What bounds it: of many rows the two passes, instructions (about 17 a token in survey, of them 12 in 64 bits) and reads
-// alike (1024 rows of 152064 fp32: 132 and 105 us, 4.7 and 5.9 TB/s; a call of 2048 such rows with filters of every kind
-// 628 us); of one row the launches and cold instructions, 27 us.  One workgroup a row, as a single launch, took 3566 us and
-// 330 us.  Calls split into groups of rows whose logits stay in the last-level cache for collect: collect is no faster, and
-// the short launches are paid for each group (797 us).
+// alike (1024 rows of 152064 fp32 with filters of every kind: 134 us, 4.6 TB/s, and 55 us for the pieces that can hold a kept
+// token; 2048 such rows 499 us); of one row the launches and cold instructions, 28 us.  One workgroup a row, as a single
+// launch, took 3566 us and 330 us.  Calls split into groups of rows whose logits stay in the last-level cache for collect:
+// collect is no faster, and the short launches are paid for each group (797 us against 628, before pieces were passed over).
 #include <algorithm>
 #include <climits>
 
@@ -35,7 +35,9 @@
 namespace {
 
 constexpr int BINS = 2048, BELOW = 33 * 16;      // bins, and those below m0
-constexpr int FEW = 4096;                        // a list of every token that may be kept is no longer
+// A list of every token that may be kept is no longer than FEW, unless top_k and top_p work together: the list of one bin
+// and the pieces' weights take less time than long lists (4096: 2048 rows 537 us, 1024: 499 us).
+constexpr int FEW = 1024;
 constexpr double UNIT = 17592186044416.0;        // 2^44
 constexpr int PIECE = 1024, PIECES = SAMPLE_MAX_VOCAB / PIECE;      // tokens whose weights are one sum of the row's
 
@@ -53,6 +55,7 @@ constexpr float MOST = 3.4028235e38f;
 
 typedef __attribute__((address_space(1))) unsigned long long* Units;
 typedef __attribute__((address_space(1))) double* Doubles;
+typedef __attribute__((address_space(1))) unsigned* Keys;
 
 template <int NT> struct Shared {
   unsigned long long mass[BINS + 64];            // (64 places for what has no bin: a lane each)
@@ -211,8 +214,8 @@ INLINE float at_least(float x, float low) {
 
 // f(logits, indexes) for the tokens [i0, i1), by the calling wave, 8 a lane at a time; i0 and i1 are the wave's.
 // A half's next loads are on their way while the other half is worked on.
-// after(i) follows each 1024 of them, from i on.
-template <class T, class F, class G> INLINE void tokens(const View<T>& v, int i0, int i1, F&& f, G&& after) {
+// after(i) follows each piece of 1024, from i on, and next(i) says where the next one is.
+template <class T, class F, class G, class X> INLINE void tokens(const View<T>& v, int i0, int i1, F&& f, G&& after, X&& next) {
   constexpr int N = View<T>::N, H = 8, P = H / N, HALF = 64 * H;
   const int lane = lane_id();
   i1 = min(i1, v.V);
@@ -225,7 +228,8 @@ template <class T, class F, class G> INLINE void tokens(const View<T>& v, int i0
   fetch(0, i0);
   fetch(1, i0 + HALF);
 #pragma unroll 1
-  for (int i = i0; i < i1; i += 2 * HALF) {
+  for (int i = i0; i < i1;) {
+    const int n = next(i);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int b = i + half * HALF;
@@ -246,13 +250,14 @@ template <class T, class F, class G> INLINE void tokens(const View<T>& v, int i0
         for (int e = 0; e < H; ++e) l[e] = index(e) < i1 ? v.logit(l[e], index(e)) : -INFINITY;
       }
       f(l, index);
-      fetch(half, b + 2 * HALF);
+      fetch(half, n + half * HALF);
     }
     after(i);
+    i = n;
   }
 }
 template <class T, class F> INLINE void tokens(const View<T>& v, int i0, int i1, F&& f) {
-  tokens(v, i0, i1, f, [](int) {});
+  tokens(v, i0, i1, f, [](int) {}, [](int i) { return i + PIECE; });
 }
 template <class T, class F> INLINE void all_tokens(const View<T>& v, F&& f) {
   const int w = wave_id();
@@ -267,13 +272,15 @@ template <int M> INLINE float largest(const float (&l)[M]) {
 }
 
 // ---- the first pass
-// Histogram of the wave's tokens [i0, i1) about m0 (counts, masses), or the weights of their pieces into seg; `top` their
-// maximum or a NaN.
-template <int MODE, int NT, class T> INLINE void survey_as(const View<T>& v, int i0, int i1, float low, float& top, Doubles seg) {
+// Histogram of the wave's tokens [i0, i1) about m0 (counts, masses) and the keys of their pieces' maxima into tops, or the
+// weights of their pieces into seg; the key of their maximum, all ones where there is a NaN.
+template <int MODE, int NT, class T> INLINE unsigned survey_as(const View<T>& v, int i0, int i1, float low, Keys tops, Doubles seg) {
   constexpr bool COUNTS = MODE & 1, MASSES = MODE & 2;
   auto& s = lds<NT>();
   const int lane = lane_id();
   double x = 0;
+  float top = -INFINITY;
+  unsigned best = 0;
   tokens(v, i0, i1, [&](auto& l, auto) __attribute__((always_inline)) {
     constexpr int M = sizeof(l) / 4;
     const float most = largest(l);
@@ -290,22 +297,27 @@ template <int MODE, int NT, class T> INLINE void survey_as(const View<T>& v, int
       if (!MODE) x += s.edge[b] * series(in_bins(p[e]) ? p[e].x : 0.0, 1.0);
     }
   }, [&](int i) __attribute__((always_inline)) {
-    if (MODE) return;
+    const unsigned t = wave_max32(top != top ? 0xffffffffu : key_of(top));
+    best = max(best, t);
+    top = -INFINITY;
+    if (MODE) {
+      if (lane == 0 && tops) tops[i / PIECE] = t;
+      return;
+    }
     x = wave_sum64(x);
     if (lane == 0) seg[i / PIECE] = x;
     x = 0;
-  });
+  }, [](int i) { return i + PIECE; });
+  return best;
 }
-// The wave's tokens [i0, i1) into the histogram, or (without counts or masses) their pieces' weights into seg; the key
-// of the workgroup's maximum, all ones where there is a NaN.
-template <int NT, class T> INLINE unsigned survey(const View<T>& v, bool masses, bool counts, int i0, int i1, Doubles seg) {
+// That of all the workgroup's tokens.
+template <int NT, class T> INLINE unsigned survey(const View<T>& v, bool masses, bool counts, int i0, int i1, Keys tops, Doubles seg) {
   const float low = v.below(0);
-  float top = -INFINITY;
-  if (masses && counts) survey_as<3, NT>(v, i0, i1, low, top, seg);
-  else if (masses) survey_as<2, NT>(v, i0, i1, low, top, seg);
-  else if (counts) survey_as<1, NT>(v, i0, i1, low, top, seg);
-  else if (seg) survey_as<0, NT>(v, i0, i1, low, top, seg);
-  return max_all<NT>(top != top ? 0xffffffffu : key_of(top));
+  return max_all<NT>(masses && counts ? survey_as<3, NT>(v, i0, i1, low, tops, seg)
+                     : masses         ? survey_as<2, NT>(v, i0, i1, low, tops, seg)
+                     : counts         ? survey_as<1, NT>(v, i0, i1, low, tops, seg)
+                     : seg            ? survey_as<0, NT>(v, i0, i1, low, tops, seg)
+                                      : 0);
 }
 
 // The largest logit of the wave's tokens [i0, i1) with its first index (key above, ~index below), or all ones for a NaN.
@@ -324,12 +336,17 @@ template <class T> INLINE unsigned long long first_token(const View<T>& v, int i
 
 // ---- the second pass
 // The wave's tokens [i0, i1) of bin b, or with ALL those of every bin from b on, to put(~key, index).  Without ALL the
-// weights of the pieces' higher bins go into seg.
-template <bool ALL, int NT, class T, class F> INLINE void collect(const View<T>& v, int b, int i0, int i1, Doubles seg, F&& put) {
+// weights of the pieces' higher bins go into seg.  Pieces whose maximum (tops) is lower are not read: 64 of them at most.
+template <bool ALL, int NT, class T, class F> INLINE void collect(const View<T>& v, int b, int i0, int i1, Keys tops, Doubles seg, F&& put) {
   auto& s = lds<NT>();
+  const int lane = lane_id(), mine = i0 + lane * PIECE;
   const float low = v.below(b);
+  const bool in = mine < min(i1, v.V), high = in && tops[in ? mine / PIECE : 0] >= key_of(low);
+  if (!ALL && in && !high) seg[mine / PIECE] = 0;
+  unsigned long long left = __ballot(high);
+  auto piece = [&] { return left ? i0 + (__ffsll(left) - 1) * PIECE : 1 << 30; };
   double x = 0;
-  tokens(v, i0, i1, [&](auto& l, auto index) __attribute__((always_inline)) {
+  tokens(v, piece(), i1, [&](auto& l, auto index) __attribute__((always_inline)) {
     constexpr int M = sizeof(l) / 4;
     if (!__ballot(largest(l) >= low)) return;
     Place p[M];
@@ -349,8 +366,11 @@ template <bool ALL, int NT, class T, class F> INLINE void collect(const View<T>&
   }, [&](int i) __attribute__((always_inline)) {
     if (ALL) return;
     x = wave_sum64(x);
-    if (lane_id() == 0) seg[i / PIECE] = x;
+    if (lane == 0) seg[i / PIECE] = x;
     x = 0;
+  }, [&](int) __attribute__((always_inline)) {
+    left &= left - 1;
+    return piece();
   });
 }
 INLINE float logit_of(unsigned long long e) { return value_of(~(unsigned)(e >> 32)); }
@@ -438,11 +458,26 @@ template <int NT> INLINE int narrow(unsigned& lo, unsigned& hi, int shift, doubl
   return n;
 }
 
+// f(element, weight) for the list's tokens: four of a thread are on their way together.
+template <int NT, class F> INLINE void each_of(const List& q, F&& f) {
+#pragma unroll 1
+  for (int i = threadIdx.x; i < q.n; i += 4 * NT) {
+    unsigned long long e[4], w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = min(i + j * NT, q.n - 1);
+      e[j] = q.e[at];
+      w[j] = q.w[at];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j * NT < q.n) f(e[j], w[j], i + j * NT);
+  }
+}
 // Weights of the list's tokens, in units of 2^-49 of w1, which none exceeds; returns the unit.
 template <int NT, class T> INLINE double list_weights(const View<T>& v, const List& q, double w1) {
   const double scale = 0x1p49 / w1;
-#pragma unroll 1
-  for (int i = threadIdx.x; i < q.n; i += NT) q.w[i] = (unsigned long long)rint(weight<NT>(v, logit_of(q.e[i])) * scale);
+  each_of<NT>(q, [&](unsigned long long e, unsigned long long, int i) { q.w[i] = (unsigned long long)rint(weight<NT>(v, logit_of(e)) * scale); });
   __syncthreads();
   return w1 * 0x1p-49;
 }
@@ -457,14 +492,13 @@ template <int NT> INLINE unsigned long long cut_in_list(const List& q, unsigned 
 #pragma unroll 1
   while (k > 1 && lo < hi) {
     const int shift = clear_parts<NT>(lo, hi);
-#pragma unroll 1
-    for (int i = tid; i < q.n; i += NT) {
-      const unsigned key = ~(unsigned)(q.e[i] >> 32);
+    each_of<NT>(q, [&](unsigned long long e, unsigned long long w, int) {
+      const unsigned key = ~(unsigned)(e >> 32);
       if (key >= lo && key <= hi) {
         atomicAdd(&s.count[(key - lo) >> shift], 1u);
-        if (!by_count) atomicAdd(&s.mass[(key - lo) >> shift], q.w[i]);
+        if (!by_count) atomicAdd(&s.mass[(key - lo) >> shift], w);
       }
-    }
+    });
     k = narrow<NT>(lo, hi, shift, above, target, by_count, unit);
   }
   // of those left, all of one value, the want-th by index: in parts of the row, the first ones highest
@@ -473,27 +507,26 @@ template <int NT> INLINE unsigned long long cut_in_list(const List& q, unsigned 
   if (k > 1) {
     double w = 1;
     if (!by_count) {
-#pragma unroll 1
-      for (int i = tid; i < q.n; i += NT)
-        if (~(unsigned)(q.e[i] >> 32) == lo) s.first = q.w[i];
+      each_of<NT>(q, [&](unsigned long long e, unsigned long long w, int) {
+        if (~(unsigned)(e >> 32) == lo) s.first = w;
+      });
       __syncthreads();
       w = (double)s.first * unit;
     }
     want = (int)fmin(fmax(1.0, ceil((target - above) / w)), (double)k);
     shift = clear_parts<NT>(0u, SAMPLE_MAX_VOCAB - 1);
-#pragma unroll 1
-    for (int i = tid; i < q.n; i += NT)
-      if (~(unsigned)(q.e[i] >> 32) == lo) atomicAdd(&s.count[BINS - 1 - ((unsigned)q.e[i] >> shift)], 1u);
+    each_of<NT>(q, [&](unsigned long long e, unsigned long long, int) {
+      if (~(unsigned)(e >> 32) == lo) atomicAdd(&s.count[BINS - 1 - ((unsigned)e >> shift)], 1u);
+    });
     double before;
     part = BINS - 1 - cross<NT>((double)want, 0.0, before);
     want -= (int)before;
   }
   __syncthreads();
-#pragma unroll 1
-  for (int i = tid; i < q.n; i += NT) {
-    const unsigned key = ~(unsigned)(q.e[i] >> 32);
-    if (key >= lo && key <= hi && (k == 1 || (unsigned)q.e[i] >> shift == (unsigned)part)) s.mass[atomicAdd(&s.n, 1)] = q.e[i];
-  }
+  each_of<NT>(q, [&](unsigned long long e, unsigned long long, int) {
+    const unsigned key = ~(unsigned)(e >> 32);
+    if (key >= lo && key <= hi && (k == 1 || (unsigned)e >> shift == (unsigned)part)) s.mass[atomicAdd(&s.n, 1)] = e;
+  });
   __syncthreads();
   const int m = s.n;
   if (tid < m) {
@@ -506,15 +539,14 @@ template <int NT> INLINE unsigned long long cut_in_list(const List& q, unsigned 
   __syncthreads();
   return e;
 }
-// the sum of f(i), i < n
-template <int NT, class F> INLINE unsigned long long sum_units(int n, F&& f) {
+// the sum of f(element, weight)
+template <int NT, class F> INLINE unsigned long long sum_units(const List& q, F&& f) {
   auto& s = lds<NT>();
   unsigned long long x = 0;
   __syncthreads();
   if (threadIdx.x == 0) s.first = 0;
   __syncthreads();
-#pragma unroll 1
-  for (int i = threadIdx.x; i < n; i += NT) x += f(i);
+  each_of<NT>(q, [&](unsigned long long e, unsigned long long w, int) { x += f(e, w); });
   if (x) atomicAdd(&s.first, x);
   __syncthreads();
   x = s.first;
@@ -541,15 +573,15 @@ INLINE void finish_list(const SampleArgs& a, const View<T>& v, const List& q, in
   for (int by = 0; by < 2; ++by) {             // top_k, then top_p
     if (by == 0 ? !(k > 0 && k < q.n) : !by_p) continue;
     double target = (double)k;
-    if (by == 1) target = p * (k > 0 ? (double)sum_units<NT>(q.n, [&](int i) { return q.e[i] <= last ? q.w[i] : 0; }) * unit : mass1);
+    if (by == 1) target = p * (k > 0 ? (double)sum_units<NT>(q, [&](unsigned long long e, unsigned long long w) { return e <= last ? w : 0; }) * unit : mass1);
     last = min(last, cut_in_list<NT>(q, lo, best, 0.0, target, by == 0, unit));
   }
   if (floor_l > -INFINITY) last = min(last, last_of(floor_l, best));
   // in the vocabulary's order: parts of the row, the first ones highest
   const int shift = clear_parts<NT>(0u, (unsigned)(v.V - 1));
-  const double total = (double)sum_units<NT>(q.n, [&](int i) {
-    const unsigned long long x = q.e[i] <= last ? q.w[i] : 0;
-    const int part = BINS - 1 - (int)((unsigned)q.e[i] >> shift);
+  const double total = (double)sum_units<NT>(q, [&](unsigned long long e, unsigned long long w) {
+    const unsigned long long x = e <= last ? w : 0;
+    const int part = BINS - 1 - (int)((unsigned)e >> shift);
     if (x) {
       atomicAdd(&s.mass[part], x);
       atomicAdd(&s.count[part], 1u);
@@ -565,9 +597,9 @@ INLINE void finish_list(const SampleArgs& a, const View<T>& v, const List& q, in
     before = -1;
   }
   // the part's tokens (no more than the row has in a part), by one wave
-#pragma unroll 1
-  for (int i = tid; i < q.n; i += NT)
-    if (q.e[i] <= last && q.w[i] && BINS - 1 - (int)((unsigned)q.e[i] >> shift) == part) s.count[atomicAdd(&s.n, 1)] = i;
+  each_of<NT>(q, [&](unsigned long long e, unsigned long long w, int i) {
+    if (e <= last && w && BINS - 1 - (int)((unsigned)e >> shift) == part) s.count[atomicAdd(&s.n, 1)] = i;
+  });
   __syncthreads();
   if (wave_id() != 0) return;
   const int m = s.n;
@@ -799,7 +831,7 @@ struct RowState {
   int mode, k, bin, n;          // n: tokens of the list
   int by_k, by_p, by_m;         // the cut's bin is that of top_k, of top_p, of min_p
 };
-constexpr int DECIDE_NT = 512;
+constexpr int DECIDE_NT = 512;      // (finish: two such workgroups fit a CU, where one of 1024 would alone: 1024 rows 50 -> 36 us)
 constexpr int LISTED = 16384, PART_LIST = 1024;      // a list's tokens in memory, and a part's of it in LDS
 
 struct Space {
@@ -807,6 +839,7 @@ struct Space {
   unsigned long long* mass;     // [rows][BINS]
   unsigned* count;              // [rows][BINS]
   double* seg;                  // [rows][PIECES]
+  unsigned* top;                // [rows][PIECES]: keys of the pieces' maxima
   double* edge;                 // [BINS]
   unsigned long long *e, *w;    // [rows][LISTED]
   int* whole;                   // how many rows are left to sample_whole, and which
@@ -919,7 +952,7 @@ template <class T> __global__ __launch_bounds__(PART_NT) void sample_survey(Call
     }
   }
   __syncthreads();
-  const unsigned best = survey<NT>(v, masses, counts, i0, i0 + share, (Doubles)(c.s.seg + (size_t)i * PIECES));
+  const unsigned best = survey<NT>(v, masses, counts, i0, i0 + share, (Keys)(c.s.top + (size_t)i * PIECES), (Doubles)(c.s.seg + (size_t)i * PIECES));
   if (tid == 0) atomicMax(&st.best, best);
   if (mode == PLAIN) return;
   for (int b = tid; b < BINS; b += NT) {
@@ -1041,8 +1074,9 @@ template <class T> __global__ __launch_bounds__(PART_NT) void sample_collect(Cal
     }
   };
   const Doubles seg = (Doubles)(c.s.seg + (size_t)i * PIECES);
-  if (mode == ALL) collect<true, NT>(v, b, i0, i0 + share, seg, put);
-  else collect<false, NT>(v, b, i0, i0 + share, seg, put);
+  const Keys tops = (Keys)(c.s.top + (size_t)i * PIECES);
+  if (mode == ALL) collect<true, NT>(v, b, i0, i0 + share, tops, seg, put);
+  else collect<false, NT>(v, b, i0, i0 + share, tops, seg, put);
   __syncthreads();
   const int m = min(n, PART_LIST);
   if (tid == 0 && m) to0 = atomicAdd(&st.n, m);
@@ -1051,8 +1085,8 @@ template <class T> __global__ __launch_bounds__(PART_NT) void sample_collect(Cal
     if (to0 + j < LISTED) out[to0 + j] = list[j];
 }
 
-template <class T> __global__ __launch_bounds__(ROW_NT) void sample_finish(Call c) {
-  constexpr int NT = ROW_NT;
+template <class T> __global__ __launch_bounds__(DECIDE_NT) void sample_finish(Call c) {
+  constexpr int NT = DECIDE_NT;
   auto& s = lds<NT>();
   const int tid = threadIdx.x, i = blockIdx.x, r = c.row0 + i;
   const RowState o = c.s.row[i];
@@ -1081,9 +1115,9 @@ template <class T> __global__ __launch_bounds__(ROW_NT) void sample_finish(Call 
     // the kept ones of the list to their pieces, in whole units
     if (tid < pieces) s.mass[tid] = 0;
     __syncthreads();
-#pragma unroll 1
-    for (int j = tid; j < q.n; j += NT)
-      if (q.e[j] <= last) atomicAdd(&s.mass[(unsigned)q.e[j] / PIECE], q.w[j]);
+    each_of<NT>(q, [&](unsigned long long e, unsigned long long w, int) {
+      if (e <= last) atomicAdd(&s.mass[(unsigned)e / PIECE], w);
+    });
     __syncthreads();
     if (tid < pieces) s.seg[tid] += (double)s.mass[tid] * unit;
     __syncthreads();
@@ -1114,7 +1148,7 @@ template <class T> INLINE void whole(const Call& c, int at) {
     __syncthreads();
     for (int b = tid; b < BINS; b += NT) s.mass[b] = s.count[b] = 0;
     __syncthreads();
-    survey<NT>(v, by || masses, !by && w.by_k, wave_id() * v.share, (wave_id() + 1) * v.share, nullptr);
+    survey<NT>(v, by || masses, !by && w.by_k, wave_id() * v.share, (wave_id() + 1) * v.share, nullptr, nullptr);
     __syncthreads();
     if (by == 0) {
       decide<NT>(v, w, masses, o.best, o);
@@ -1161,6 +1195,7 @@ size_t carve(Space& s, char* p, long rows) {
   s.mass = (unsigned long long*)take(rows * BINS * 8);
   s.count = (unsigned*)take(rows * BINS * 4);
   s.seg = (double*)take(rows * PIECES * 8);
+  s.top = (unsigned*)take(rows * PIECES * 4);
   s.edge = (double*)take(BINS * 8);
   s.e = (unsigned long long*)take((size_t)rows * LISTED * 8);
   s.w = (unsigned long long*)take((size_t)rows * LISTED * 8);
@@ -1175,8 +1210,9 @@ template <class T> void launch_t(const SampleArgs& a, void* workspace, hipStream
   for (long row0 = 0; row0 < a.rows; row0 += group) {
     const int rows = (int)std::min<long>(group, a.rows - row0);
     c.row0 = (int)row0;
-    // a part is no shorter than 4096 tokens, and there are no more of them than fill the GPU a few times over
-    const long parts = std::max(1l, std::min(4096l / rows, (a.vocab + 4095l) / 4096));
+    // a part is no shorter than 4096 tokens (a wave of it a piece), and there are about as many as the GPU holds at once or
+    // twice as many: 6 of survey's workgroups on a CU (2048 rows: 628 us with 4096 parts a group, 652 with 2048, 537 with 3072)
+    const long parts = std::max(1l, std::min(3072l / rows, (a.vocab + 4095l) / 4096));
     c.part = (int)((a.vocab + parts - 1) / parts + 4095) / 4096 * 4096;
     c.parts = (a.vocab + c.part - 1) / c.part;
     const dim3 grid((unsigned)c.parts, (unsigned)rows);
@@ -1184,7 +1220,7 @@ template <class T> void launch_t(const SampleArgs& a, void* workspace, hipStream
     sample_survey<T><<<grid, PART_NT, 0, st>>>(c);
     sample_decide<T><<<rows, DECIDE_NT, 0, st>>>(c);
     sample_collect<T><<<grid, PART_NT, 0, st>>>(c);
-    sample_finish<T><<<rows, ROW_NT, 0, st>>>(c);
+    sample_finish<T><<<rows, DECIDE_NT, 0, st>>>(c);
     sample_whole<T><<<std::min(rows, 256), ROW_NT, 0, st>>>(c);
   }
 }
