@@ -10,35 +10,41 @@
 //   code  nearest e4m3 value of x / 2^e, ties to the even code; saturates where e is clamped
 // and the whole block is written (zeros behind the last row).  All of it is exact in fp32 but
 // the rounding, which is the hardware's own conversion.
+//
+// What bounds them: memory.  21500 rows of 32 heads of 128 in fp16, with pages of 64: the keys are stored in 60 us (4.4 TB/s of
+// rows and codes), the transposed values in 62, all are read back in 115 (4.6 TB/s).
 #include <algorithm>
+#include <climits>
 
 #include "cache8.h"
 
 namespace {
 
 constexpr int NT = 256;
-constexpr int UNIT = 2 * C8_BLOCK;          // tokens of a workgroup: 128 bytes of a transposed row in fp16
+constexpr int UNIT = 2 * C8_BLOCK;          // tokens of a storing workgroup
+constexpr int LONG_UNIT = 128;              // of one that stores transposed values: the consecutive ones that it reads of a dimension
 
 typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // inclusive sum over the wave's lanes
 __device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(x, o, 64);
-    if (lane >= o) x += t;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8, row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
 
-// The 64-token units of the batch, in sequence order: unit `key` is unit `first` + n of sequence b.
+// The batch's units of U tokens, in sequence order: unit `key` is unit `first` + n of sequence b.
 struct Span {
-  int b, start, row0, row1, unit;   // rows row0 .. row1 - 1 at positions start ..; unit: number of the 64 tokens
+  int b, start, row0, row1, unit;   // rows row0 .. row1 - 1 at positions start ..; unit: number of the U tokens
 };
-__device__ __forceinline__ Span find_unit(const C8WriteArgs& a, int key) {
+template <int U> __device__ __forceinline__ Span find_unit(const C8WriteArgs& a, int key) {
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -47,7 +53,7 @@ __device__ __forceinline__ Span find_unit(const C8WriteArgs& a, int key) {
     const int s = a.start[b], r0 = min(max(a.row_off[b], 0), a.rows), r1 = min(max(a.row_off[b + 1], r0), a.rows);
     const long long cap = (long long)a.width << a.c.psh;
     const int fit = s < 0 ? 0 : (int)min((long long)(r1 - r0), max(cap - s, 0LL));
-    const int n = b0 + lane < a.batch && fit > 0 ? (int)(((long long)s + fit - 1) / UNIT) - s / UNIT + 1 : 0;
+    const int n = b0 + lane < a.batch && fit > 0 ? (int)(((long long)s + fit - 1) / U) - s / U + 1 : 0;
     const int incl = wave_scan(n);
     const unsigned long long m = __ballot(base + incl > key);
     if (m) {
@@ -57,7 +63,7 @@ __device__ __forceinline__ Span find_unit(const C8WriteArgs& a, int key) {
       v.start = __builtin_amdgcn_readlane(s, at);
       v.row0 = __builtin_amdgcn_readlane(r0, at);
       v.row1 = v.row0 + __builtin_amdgcn_readlane(fit, at);
-      v.unit = v.start / UNIT + key - (base + __builtin_amdgcn_readlane(incl - n, at));
+      v.unit = v.start / U + key - (base + __builtin_amdgcn_readlane(incl - n, at));
       return v;
     }
     base += __builtin_amdgcn_readlane(incl, 63);
@@ -88,22 +94,19 @@ __device__ __forceinline__ void unpack4(float* x, unsigned c, float sc) {
 // N consecutive elements, aligned to an element
 template <int N, class T> __device__ __forceinline__ void load_n(T (&x)[N], const T* p) { __builtin_memcpy(x, p, N * sizeof(T)); }
 
-// A workgroup's two blocks.  TRANS: a head's values lie with their rows one element apart.
-//   keys          thread: row tid / 8 of each block, HD / 8 dimensions from (tid % 8) HD / 8
-//   values        wave w: 8-token block w of each block; lane (of HD / 2): dimensions 2 lane, 2 lane + 1
-//   transposed    the same shares; lane l of wave w has 8-token block l % 4, so that the four
-//                 lanes of a dimension read 64 consecutive bytes
-template <class T, int HD, int KIND>     // 0 keys, 1 values, 2 values transposed
+// A workgroup's two blocks.
+//   keys     thread: row tid / 8 of each block, HD / 8 dimensions from (tid % 8) HD / 8
+//   values   wave w: 8-token block w of each block; lane (of HD / 2): dimensions 2 lane, 2 lane + 1
+template <class T, int HD, int KIND>     // 0 keys, 1 values
 __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, int h) {
   using L = C8<HD>;
   constexpr int E = HD / 8, NB = UNIT / C8_BLOCK;       // elements of a thread of a block (values: 16, of fewer threads)
   constexpr int EV = KIND == 0 ? E : 16;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, Tp = 1 << a.c.psh;
   const T* src = KIND == 0 ? (const T*)a.K + h * a.k_head : (const T*)a.V + h * a.v_head;
-  const bool on = KIND == 0 || HD == 128 || (KIND == 1 ? lane < HD / 2 : w < 2);
+  const bool on = KIND == 0 || HD == 128 || lane < HD / 2;
   // a thread's 8-token block and first dimension of its pair (values)
-  const int tb = KIND == 1 ? w : lane & 3, pair = KIND == 1 ? lane : (lane >> 2) + 16 * w;
-  const int dim = KIND == 0 ? (tid & 7) * E : 2 * min(pair, HD / 2 - 1);
+  const int tb = w, dim = KIND == 0 ? (tid & 7) * E : 2 * min(lane, HD / 2 - 1);
   const int n = v.row1 - v.row0, end = v.start + n;
   float x[NB][EV];
   unsigned top[NB], old[NB];          // old: scale byte of a block that is joined, else 0
@@ -126,29 +129,13 @@ __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, 
     auto row = [&](int i) __attribute__((always_inline)) { return (long)v.row0 + min(max(p0 + i - v.start, 0), n - 1); };
     if constexpr (KIND == 0) {
       load_n<EV>(t[k], src + row(tid >> 3) * a.k_row + dim);
-    } else if constexpr (KIND == 1) {
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         T y[2];
         load_n<2>(y, src + row(8 * tb + i) * a.v_row + dim);
         t[k][i] = y[0];
         t[k][8 + i] = y[1];
-      }
-    } else {
-      const int q = p0 + 8 * tb - v.start;
-      if (q >= 0 && q + 8 <= n) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          T y[8];
-          load_n<8>(y, src + (dim + s) * a.v_dim + v.row0 + q);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) t[k][8 * s + i] = y[i];
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) t[k][8 * s + i] = src[(dim + s) * a.v_dim + row(8 * tb + i)];
       }
     }
   }
@@ -209,43 +196,273 @@ __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, 
   }
 }
 
-template <class T, int HD, bool VT>
+template <class T, int HD>
 __global__ __launch_bounds__(NT) void cache8_write_kernel(C8WriteArgs a) {
-  const Span v = find_unit(a, blockIdx.x);
+  const Span v = find_unit<UNIT>(a, blockIdx.x);
   if (v.b < 0) return;
   if (blockIdx.z == 0) write_unit<T, HD, 0>(a, v, blockIdx.y);
-  else write_unit<T, HD, VT ? 2 : 1>(a, v, blockIdx.y);
+  else write_unit<T, HD, 1>(a, v, blockIdx.y);
 }
 
-// Read back: a thread 8 dimensions of a row.  A slot outside the cache gives zeros.
+// Two dimensions of 8 tokens.  `in`: all ones in the halves of tokens that count, two a word.
+template <class T> struct Pair {
+  float x[16];
+  __device__ __forceinline__ void load(int s, const float* p) { __builtin_memcpy(&x[8 * s], p, 32); }
+  __device__ __forceinline__ void set(int e, float y) { x[e] = y; }
+  static __device__ __forceinline__ bool has(const unsigned (&in)[4], int e) { return in[e % 8 / 2] >> (e % 2 * 16) & 1; }
+  __device__ __forceinline__ void keep(const unsigned (&in)[4]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = has(in, e) ? x[e] : 0.f;
+  }
+  __device__ __forceinline__ float largest() const {       // of |x|; a NaN is none
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
+    return m;
+  }
+  __device__ __forceinline__ void join(const unsigned (&c)[4], float sc, const unsigned (&in)[4]) {      // stored tokens
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      float y[4];
+      unpack4(y, c[e / 4], sc);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[e + j] = has(in, e + j) ? y[j] : x[e + j];
+    }
+  }
+  __device__ __forceinline__ void clamp(float most) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = x[e] > most ? most : x[e] < -most ? -most : x[e];
+  }
+  __device__ __forceinline__ u32x4 codes(float sc) const { return u32x4{pack4(x, sc), pack4(x + 4, sc), pack4(x + 8, sc), pack4(x + 12, sc)}; }
+};
+// in fp16 two elements to an instruction; every stored element is one of fp16
+template <> struct Pair<f16> {
+  unsigned x[8];
+  static __device__ __forceinline__ unsigned bits(f16 y) { return __builtin_bit_cast(unsigned short, y); }
+  __device__ __forceinline__ void load(int s, const f16* p) { __builtin_memcpy(&x[4 * s], p, 16); }
+  __device__ __forceinline__ void set(int e, f16 y) { x[e / 2] = e % 2 ? x[e / 2] | bits(y) << 16 : bits(y); }      // (in order)
+  __device__ __forceinline__ void keep(const unsigned (&in)[4]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] &= in[i % 4];
+  }
+  __device__ __forceinline__ float largest() const {
+    u16x2 m = {0, 0};                      // the bits of |x| are ordered as it is, NaNs above all
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+    unsigned t = max(m[0], m[1]);
+    if (__ballot(t > 0x7c00)) {
+      t = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 32; j += 16) {
+          const unsigned y = x[i] >> j & 0x7fff;
+          t = y <= 0x7c00 ? max(t, y) : t;
+        }
+    }
+    return (float)__builtin_bit_cast(f16, (unsigned short)t);
+  }
+  __device__ __forceinline__ void join(const unsigned (&c)[4], float sc, const unsigned (&in)[4]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const f16x2 y = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i / 2], sc, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i / 2], sc, false);
+      x[i] = (x[i] & ~in[i % 4]) | (__builtin_bit_cast(unsigned, y) & in[i % 4]);
+    }
+  }
+  __device__ __forceinline__ void clamp(float most) {      // (most is 448 * 2^7 = 57344)
+    const unsigned top = bits((f16)most);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      unsigned y = 0;
+#pragma unroll
+      for (int j = 0; j < 32; j += 16) {
+        const unsigned v = x[i] >> j & 0xffff, m = v & 0x7fff;
+        y |= (m <= 0x7c00 && m > top ? (v & 0x8000) | top : v) << j;
+      }
+      x[i] = y;
+    }
+  }
+  __device__ __forceinline__ u32x4 codes(float sc) const {
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      i16x2 r = {0, 0};
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, x[2 * i]), sc, false);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, x[2 * i + 1]), sc, true);
+      c[i] = __builtin_bit_cast(unsigned, r);
+    }
+    return c;
+  }
+};
+
+// Transposed values.  A wave has HD / waves dimensions, two groups of two a lane; lane l 8-token block l % BLOCKS, so that
+// BLOCKS lanes read the unit's tokens of a dimension.  Codes go by LDS, as a lane's 16 bytes are apart from the next one's.
+// (The time goes with the instructions: 106 us where every element was widened to fp32 and the codes' places were found per
+// lane.  Units of 64 tokens and no LDS 125 us, of 256 tokens 129.)
 template <class T, int HD>
-__global__ __launch_bounds__(NT) void cache8_read_kernel(C8ReadArgs a) {
-  constexpr int U = HD / 8, VF = HD / 16;
+__global__ __launch_bounds__(LONG_UNIT * 4) void cache8_write_long_kernel(C8WriteArgs a) {
   using L = C8<HD>;
-  const int u = threadIdx.x % U, h = blockIdx.y, T_ = 1 << a.c.psh;
-  const long r = (long)blockIdx.x * (NT / U) + threadIdx.x / U;
+  constexpr int LNT = LONG_UNIT * 4, NW = LNT / 64, BLOCKS = LONG_UNIT / 8, SCALES = LONG_UNIT / C8_BLOCK;
+  constexpr int NI = HD / 64;                            // items of a thread: two dimensions of 8 tokens
+  constexpr int PITCH = L::VBLK + 16;
+  __shared__ unsigned red[SCALES][NW];
+  __shared__ alignas(16) uint8_t tile[BLOCKS * PITCH];
+  const Span v = find_unit<LONG_UNIT>(a, blockIdx.x);
+  if (v.b < 0) return;
+  const int h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6, Tp = 1 << a.c.psh;
+  const T* src = (const T*)a.V + h * a.v_head;
+  const int tb = lane % BLOCKS, n = v.row1 - v.row0, end = v.start + n, u0 = v.unit * LONG_UNIT, p = u0 + tb * 8, q = p - v.start;
+  auto dim = [&](int i) __attribute__((always_inline)) { return HD / NW * w + 2 * (NI * (lane / BLOCKS) + i); };
+  // every row is requested before the first is looked at; rows that are not the sequence's read its first or last one
+  Pair<T> t[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const T* from = src + (dim(i) + s) * a.v_dim + v.row0;
+      if (q >= 0 && q + 8 <= n) {
+        t[i].load(s, from + q);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[i].set(8 * s + j, from[min(max(q + j, 0), n - 1)]);
+      }
+    }
+  }
+  // where block k of the unit is, or null
+  auto head = [&](int k) __attribute__((always_inline)) -> uint8_t* {
+    const int p0 = u0 + k * C8_BLOCK, pg = a.table[(size_t)v.b * a.width + min(p0 >> a.c.psh, a.width - 1)];
+    const bool ok = pg >= 0 && pg < a.c.n_pages && p0 < end && p0 + C8_BLOCK > v.start;
+    return ok ? a.c.data + ((size_t)pg * a.c.hkv + h) * L::page_bytes(Tp) : nullptr;
+  };
+  const int k = tb / 4, p0 = u0 + k * C8_BLOCK;          // the lane's block of a scale
+  uint8_t* const page = head(k);
+  uint8_t* const scale = page + L::soff(Tp) + ((p0 & (Tp - 1)) >> 5) * 2 + 1;
+  unsigned old = 0;                                      // scale byte of a block that is joined
+  if (page && p0 < v.start) old = min(max((unsigned)*scale, (unsigned)C8_EMIN), (unsigned)C8_EMAX);
+  auto tokens = [&](int from, int to, unsigned (&in)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = p + 2 * j;
+      in[j] = (at >= from && at < to ? 0xffffu : 0u) | (at + 1 >= from && at + 1 < to ? 0xffff0000u : 0u);
+    }
+  };
+  if (u0 < v.start || u0 + LONG_UNIT > end) {
+    unsigned in[4];
+    tokens(v.start, end, in);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) t[i].keep(in);
+  }
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) m = fmaxf(m, t[i].largest());
+#pragma unroll
+  for (int o = 1; o < 64; o = o == 2 ? BLOCKS : 2 * o) m = fmaxf(m, __shfl_xor(m, o, 64));      // over the block's lanes
+  if (lane < BLOCKS && lane % 4 == 0) red[k][w] = __float_as_uint(m);
+  __syncthreads();                                       // (scales are read before they are written, too)
+  unsigned top = 0;
+#pragma unroll
+  for (int j = 0; j < NW; ++j) top = max(top, red[k][j]);
+  const unsigned eb = max(exponent_of(top), old);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int off = dim(i) % (HD / 16) / 2 * 256 + dim(i) / (HD / 16) * 16;
+    if (old) {
+      unsigned c[4], in[4];
+      __builtin_memcpy(c, __builtin_assume_aligned(page + L::voff(Tp) + ((p & (Tp - 1)) >> 3) * L::VBLK + off, 16), 16);
+      tokens(INT_MIN, v.start, in);
+      t[i].join(c, scale_of(old), in);
+    }
+    if (eb == (unsigned)C8_EMAX) t[i].clamp(448.f * scale_of(eb));      // only here can an element lie beyond 448
+    *(u32x4*)(tile + tb * PITCH + off) = t[i].codes(scale_of(eb));
+  }
+  if (page && w == 0 && lane < BLOCKS && lane % 4 == 0) *scale = (uint8_t)eb;
+  __syncthreads();
+  constexpr int PIECES = L::VBLK / 16;
+#pragma unroll
+  for (int i = tid; i < BLOCKS * PIECES; i += LNT) {
+    const int b = i / PIECES, piece = i % PIECES * 16;
+    uint8_t* to = head(__builtin_amdgcn_readfirstlane(b / 4));      // (64 / PIECES 8-token blocks of a wave)
+    if (to) *(u32x4*)(to + L::voff(Tp) + (((u0 + b * 8) & (Tp - 1)) >> 3) * L::VBLK + piece) = *(const u32x4*)(tile + b * PITCH + piece);
+  }
+}
+
+// Read back.  A slot outside the cache gives zeros.
+//   keys    a thread 8 dimensions of a row
+//   values  8 rows of HD / 2 lanes, two dimensions each.  Where the slots follow each other in one page, the
+//           codes are those of two 8-token blocks at most, 16 bytes a lane each: shifted to begin at the first row,
+//           two dimensions' codes of a row side by side.  Else byte by byte (all of them: 165 us with the keys, not 115).
+template <class T> __device__ __forceinline__ void put2(T* out, unsigned c, bool high, float sc) {      // (its low or high half)
+  if constexpr (sizeof(T) == 2) {
+    const f16x2 y = high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, sc, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, sc, false);
+    *(unsigned*)out = __builtin_bit_cast(unsigned, y);
+  } else {
+    *(f32x2*)out = high ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, sc, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, sc, false);
+  }
+}
+template <class T, int HD> __device__ __forceinline__ void read_values(const C8ReadArgs& a, long r0, int h) {
+  using L = C8<HD>;
+  constexpr int G = HD / 2, VF = HD / 16;                  // lanes of 8 rows
+  const int lane = threadIdx.x & 63, p = lane % G, j = lane & 7, T_ = 1 << a.c.psh;
+  r0 += lane / G * 8;
+  const long all = (long)a.c.n_pages << a.c.psh;
+  const int slot = a.slots[min(r0 + j, (long)a.rows - 1)], first = __shfl(slot, lane - p, 64), t0 = first & (T_ - 1);
+  const bool follows = (long)slot == (long)first + j && first >= 0 && first + 7L < all && t0 + 7 < T_ && r0 + 7 < a.rows;
+  const bool run = (__ballot(follows) >> (lane - p) & 0xff) == 0xff;
+  const int d = 2 * p, off = d % VF / 2 * 256 + d / VF * 16;      // of the lane's two dimensions in an 8-token block
+  auto head = [&](int s) __attribute__((always_inline)) { return a.c.data + ((size_t)(s >> a.c.psh) * a.c.hkv + h) * L::page_bytes(T_); };
+  T* out = (T*)a.Vo + ((size_t)h * a.rows + r0) * HD + d;
+  if (run) {
+    const uint8_t* page = head(first);
+    const uint8_t* codes = page + L::voff(T_) + (t0 >> 3) * L::VBLK + off;
+    u32x4 lo = *(const u32x4*)codes, hi = lo;
+    const int o = t0 & 7;
+    if (o) hi = *(const u32x4*)(codes + L::VBLK);
+    unsigned c[4];                                         // tokens 0 .. 3 of either dimension, then 4 .. 7
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      unsigned long long x = (unsigned long long)lo[2 * s + 1] << 32 | lo[2 * s];
+      const unsigned long long y = (unsigned long long)hi[2 * s + 1] << 32 | hi[2 * s];
+      if (o) x = x >> (8 * o) | y << (64 - 8 * o);
+      c[s] = (unsigned)x;
+      c[2 + s] = (unsigned)(x >> 32);
+    }
+    const uint8_t* scales = page + L::soff(T_) + 1;
+    const float s0 = scale_of(scales[(t0 >> 5) * 2]), s1 = scale_of(scales[((t0 + 7) >> 5) * 2]);
+    const int more = 32 - (t0 & 31);                       // rows of the first scale
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      // (dimension 0, dimension 1) of two rows
+      const unsigned y = __builtin_amdgcn_perm(c[i / 4 * 2 + 1], c[i / 4 * 2], i % 4 ? 0x07030602u : 0x05010400u);
+      put2(out + (size_t)i * HD, y, false, i < more ? s0 : s1);
+      put2(out + (size_t)(i + 1) * HD, y, true, i + 1 < more ? s0 : s1);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (r0 + i >= a.rows) break;
+    const int s = a.slots[r0 + i];
+    const bool ok = s >= 0 && s < all;
+    const int t = ok ? s & (T_ - 1) : 0;
+    const uint8_t* page = head(ok ? s : 0);
+    const uint8_t* codes = page + L::voff(T_) + (t >> 3) * L::VBLK + off + (t & 7);
+    const unsigned y = codes[0] | (unsigned)codes[8] << 8;
+    const float sc = scale_of(page[L::soff(T_) + (t >> 5) * 2 + 1]);
+    put2(out + (size_t)i * HD, ok ? y : 0u, false, ok ? sc : 1.f);
+  }
+}
+template <class T, int HD> __device__ __forceinline__ void read_keys(const C8ReadArgs& a, long r, int u, int h) {
+  using L = C8<HD>;
   if (r >= a.rows) return;
-  const bool value = blockIdx.z != 0;
-  const int slot = a.slots[r];
+  const int T_ = 1 << a.c.psh, slot = a.slots[r];
   const bool ok = slot >= 0 && slot < (long)a.c.n_pages << a.c.psh;
   const int s = ok ? slot : 0, t = s & (T_ - 1);
   const uint8_t* page = a.c.data + ((size_t)(s >> a.c.psh) * a.c.hkv + h) * L::page_bytes(T_);
-  unsigned c[2] = {0, 0};
-  if (!value) {
-    const u32x2 k = *(const u32x2*)(page + (size_t)t * HD + u * 8);
-    c[0] = k[0];
-    c[1] = k[1];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = u * 8 + e;
-      c[e >> 2] |= (unsigned)page[L::voff(T_) + (t >> 3) * L::VBLK + d % VF / 2 * 256 + d / VF * 16 + d % 2 * 8 + (t & 7)] << (8 * (e & 3));
-    }
-  }
-  const unsigned eb = page[L::soff(T_) + (t >> 5) * 2 + value];
+  u32x2 c = *(const u32x2*)(page + (size_t)t * HD + u * 8);
+  const unsigned eb = page[L::soff(T_) + (t >> 5) * 2];
   if (!ok) c[0] = c[1] = 0;
   const float sc = scale_of(ok ? eb : 127u);
-  T* out = (T*)(value ? a.Vo : a.Ko) + ((size_t)h * a.rows + r) * HD + u * 8;
+  T* out = (T*)a.Ko + ((size_t)h * a.rows + r) * HD + u * 8;
   if constexpr (sizeof(T) == 2) {
     u32x4 y;
 #pragma unroll
@@ -262,20 +479,34 @@ __global__ __launch_bounds__(NT) void cache8_read_kernel(C8ReadArgs a) {
     *(f32x4*)(out + 4) = f32x4{y[4], y[5], y[6], y[7]};
   }
 }
+constexpr int READ_ROWS = 64;      // rows of a workgroup
+template <class T, int HD>
+__global__ __launch_bounds__(NT) void cache8_read_kernel(C8ReadArgs a) {
+  constexpr int U = HD / 8, W = NT / 64, V = 8 * 128 / HD;      // rows of a wave (values)
+  const long r0 = (long)blockIdx.x * READ_ROWS;
+  const int h = blockIdx.y;
+  if (blockIdx.z == 0) {
+#pragma unroll
+    for (int i = 0; i < READ_ROWS; i += NT / U) read_keys<T, HD>(a, r0 + i + threadIdx.x / U, threadIdx.x % U, h);
+  } else {
+#pragma unroll
+    for (int i = 0; i < READ_ROWS; i += V * W) read_values<T, HD>(a, r0 + i + (threadIdx.x >> 6) * V, h);
+  }
+}
 
 template <class T, int HD>
 void write_t(const C8WriteArgs& a, hipStream_t st) {
-  // a sequence of n rows touches at most (n + 126) / 64 units, and no more than n
-  const long units = std::min((long)a.rows, a.rows / UNIT + 2L * a.batch);
-  const dim3 grid((unsigned)units, (unsigned)a.c.hkv, 2);
-  if (a.v_dim == 1) cache8_write_kernel<T, HD, false><<<grid, NT, 0, st>>>(a);
-  else cache8_write_kernel<T, HD, true><<<grid, NT, 0, st>>>(a);
+  // a sequence of n rows touches at most (n + 2 U - 2) / U units of U, and no more than n
+  auto units = [&](int u) { return (unsigned)std::min((long)a.rows, a.rows / u + 2L * a.batch); };
+  const unsigned heads = (unsigned)a.c.hkv;
+  const bool transposed = a.v_dim != 1;
+  cache8_write_kernel<T, HD><<<dim3(units(UNIT), heads, transposed ? 1 : 2), NT, 0, st>>>(a);
+  if (transposed) cache8_write_long_kernel<T, HD><<<dim3(units(LONG_UNIT), heads), LONG_UNIT * 4, 0, st>>>(a);
 }
 
 template <class T, int HD>
 void read_t(const C8ReadArgs& a, hipStream_t st) {
-  constexpr int per = NT / (HD / 8);
-  const dim3 grid((unsigned)((a.rows + (long)per - 1) / per), (unsigned)a.c.hkv, 2);
+  const dim3 grid((unsigned)((a.rows + READ_ROWS - 1L) / READ_ROWS), (unsigned)a.c.hkv, 2);
   cache8_read_kernel<T, HD><<<grid, NT, 0, st>>>(a);
 }
 

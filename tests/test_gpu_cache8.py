@@ -108,6 +108,24 @@ def test_read_of_any_bytes(dtype, hd):
         np.testing.assert_array_equal(host(got), ref)
 
 
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("hd,page", [(64, 32), (128, 64)])
+def test_read_of_runs(dtype, hd, page):
+    """Slots that follow each other from every place in a block, over pages' ends and out of the cache, and some that do not quite."""
+    rng = np.random.default_rng(7)
+    H, n_pages = 3, 5
+    data = random_bytes(rng, n_pages, H, page, hd)
+    data[:, :, 2 * page * hd:] = rng.integers(112, 135, data[:, :, 2 * page * hd:].shape)
+    n = n_pages * page
+    runs = [np.arange(o, o + 57) for o in range(8)] + [np.arange(n - 50, n + 9), np.arange(-9, 20), np.arange(40)[::-1], np.repeat(3, 16)]
+    odd = np.arange(64)
+    odd[[5, 17, 29, 63]] = [6, 16, -1, n]
+    slots = np.concatenate(runs + [odd, np.arange(2 * page - 3, 2 * page + 2)])
+    k, v = archer().cache8_read(new_cache(data, page, hd), dev_i32(slots), dtype)
+    for got, ref in zip((k, v), o8.read(data, page, hd, slots)):
+        np.testing.assert_array_equal(host(got), ref)
+
+
 def test_every_fp32_rounding_of_a_scale():
     """All codes, all midpoints and their neighbours, at every scale, through a store."""
     m = o8.MAGNITUDES
