@@ -149,18 +149,18 @@ template <int HD> struct Fmt8 {
 // Which kernel a call takes, by its number of columns (us on a GPU of 256 CUs, cached +
 // fresh keys, heads of 128 dimensions, unless said otherwise):
 //   COL1: up to 16 columns of a key head, a block to a workgroup.
-//   COL2: more of them.  Against one block, it expands a step for 32 columns; against four
-//     (64), two waves fit a SIMD: B 32, 2000 + 8 keys, 8 rows, 28/4 heads: 18.5, four 28.4.
-//   WIDE: columns enough that a workgroup's 256 (head_dim 128, row kernel) or 4 x 64
-//     (head_dim 64, four blocks a wave) occupy half of the CUs, or all of them twice:
-//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   153   COL2 208
-//       B  8, 512 + 256,       256,      32/32          41         64
-//       B 16, 1000 + 128,      128,      16/16          35         39
-//       B  4, 512 + 256,       256,      32/32          34         34
-//       B  2, 4096 + 256,      256,      32/32         117         54    (so not here)
-//       B  8, 1024 + 70,        70,      32/32          32         29    (nor here)
-//       B 16, 1344 + 256,      256,      32/32, 64 dim. 83         98
-//       B  8, 512 + 256,       256,      16/16, 64 dim. 27         19    (nor here)
+//   COL2: more of them.  Against one block, it expands a step for 32 columns: B 32, 2000 + 8
+//     keys, 8 rows, 28/4 heads: 24.1, one block 25.7.
+//   WIDE: columns enough that the row kernel's workgroups of 256 occupy half of the CUs:
+//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   114   COL2 198
+//       B 16, 1000 + 128,      128,      16/16          34         38
+//       B  8, 1000 + 128,      128,      32/32          35         39
+//       B  4, 512 + 256,       256,      32/32          31         37
+//       B  4, 1000 + 192,      192,      32/32          42         34    (so not here)
+//       B  2, 4096 + 256,      256,      32/32         116         53    (nor here)
+//       B  8, 1000 + 96,       96,       32/32          34         30    (nor here)
+//     With 64 dimensions four blocks of columns a wave take longer than two (B 16, 1344 + 256 keys,
+//     256 rows, 32/32 heads: 111, two 79), whatever the batch.
 enum class Kind { COL1, COL2, WIDE };
 Kind kind_of(int fp32, int batch, int G, int hq, int hkv, int hd) {
   const long ncol = (long)G * (hq / hkv), all = ncol * batch * hkv;
@@ -169,7 +169,7 @@ Kind kind_of(int fp32, int batch, int G, int hq, int hkv, int hd) {
   if (fp32 || ncol <= 16) return Kind::COL1;
   // at least half of the 256 columns of the workgroups in use
   const bool full = (ncol + 31) / 32 >= 4 * ((ncol + 255) / 256);
-  return full && all >= (hd == 128 ? 1 << 15 : 1 << 16) ? Kind::WIDE : Kind::COL2;
+  return hd == 128 && full && all >= 1 << 15 ? Kind::WIDE : Kind::COL2;
 }
 
 template <class T, int HD>
@@ -178,16 +178,18 @@ void launch_kind(PagedAttnArgs a, hipStream_t st) {
   const long ncol = (long)a.G * (a.hq / a.hkv), cols = kind == Kind::COL1 ? 16 : kind == Kind::COL2 ? 32 : 256;
   const dim3 grid((unsigned)(a.hkv * ((ncol + cols - 1) / cols)), (unsigned)a.slots);
   // More workgroups than CUs: the longest sequences first, or the last ones to start are waited
-  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 155 us, not 166).  In the
-  // column kernel, several to a CU and shorter, it costs more than it gives (64 of 512 + 32
-  // keys, 32 rows, 32 heads: 65 us, not 54).
+  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 106 us, not 126).  In the
+  // column kernel, several to a CU and shorter, it gives nothing (64 of 512 + 32 keys, 32 rows, 32 heads: 73 us, 72).
   a.sorted = kind == Kind::WIDE && a.batch > 1 && (long)grid.x * a.batch > 256;
   if (kind == Kind::COL1) {
     paged_columns_kernel<Fmt8<HD>, T, HD, 1, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
   } else if constexpr (sizeof(T) == 2) {
-    if (kind == Kind::COL2) paged_columns_kernel<Fmt8<HD>, T, HD, 2, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
-    else if constexpr (HD == 128) paged_rows_kernel<Fmt8<HD>><<<grid, 64 * RW, 0, st>>>(a);
-    else paged_columns_kernel<Fmt8<HD>, T, HD, 4, 1><<<grid, 64 * NWAVE, 0, st>>>(a);
+    if constexpr (HD == 128) {
+      if (kind == Kind::WIDE) paged_rows_kernel<Fmt8<HD>><<<grid, 64 * RW, 0, st>>>(a);
+      else paged_columns_kernel<Fmt8<HD>, T, HD, 2, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
+    } else {
+      paged_columns_kernel<Fmt8<HD>, T, HD, 2, NWAVE><<<grid, 64 * NWAVE, 0, st>>>(a);
+    }
   }
   if (a.slots > a.batch) {
     constexpr int SL = 256 / (HD / 4);
@@ -199,46 +201,49 @@ void launch_kind(PagedAttnArgs a, hipStream_t st) {
 
 }  // namespace
 
-// A workgroup of four waves takes about 0.13 us for a step of its sequence, and about 160 of
-// them together what the memory (one block) or the CUs (two) can do.  Cutting the sequences
-// costs the merge's launch and a second pass over the queries, 4 to 8 us (part of it the merge's own
-// scan of the lengths), so it has to save more than 56 steps.  Unsplit and split:
-//   B  1,  2500 keys,  1 row, 32/8 heads    13.9   15.0
-//   B  4,  2500,       1,     32/8          14.7   13.7
-//   B  4,  4096,       1,     32/8          20.9   14.7
-//   B 32,  2500,       1,     32/8          18.4   22.8
-//   B  8,  2000 + 8,   8,     28/4          16.8   20.6
+// A workgroup of four waves takes 0.14 us for a step of its sequence (64 dimensions 0.09, fp32 0.61 and 0.33): expansion and
+// matrix instructions fill its CU, and eight or sixteen waves take as long.  90 workgroups (123) reach what the memory
+// gives, in fp32 it takes all of the CUs.  Cutting the sequences costs the merge's launch and a second pass over the
+// queries, about 5 us.  So it has to save more steps than that is.  Unsplit and split, one row of 28/4 heads:
+//                      128 dimensions   64           fp32
+//   B  1,  1000 keys    8.4   10.1       6.2    9.2   23.5   14.1
+//   B  1,  2000        12.8   10.1       9.3    9.4   43.0   14.1
+//   B  4,  4000        21.6   10.7      15.1    9.8   81.4   14.4
+//   B 16,  2000        13.3   12.8       9.5   11.1   43.4   19.5
+//   B 16,  4000        22.1   17.7      15.7   13.4   82.1   30.6
+//   B 32,  2000        14.1   17.5       9.9   13.3   43.2   33.2
 // That is for sequences of one length, which is all that the host knows.  Where one of them may be
-// far longer, its workgroup alone may walk for long, so a call of more than 1024 steps (130 us)
+// far longer, its workgroup alone may walk for long, so a call of more than 1024 steps (140 us)
 // is cut whatever the batch would take together; the chunks are made of the lengths there are, about
 // one to a sequence where these are alike.  Up to 256 sequences: every wave scans their lengths.  Not where the
 // key heads and blocks of one sequence are a round of workgroups by themselves (the partial results
-// are twice its queries): there is nothing to gain (fp32, 128 rows, 32/32 heads, half a round: 1048, 1025).
+// are twice its queries): there is nothing to gain.
 //                                           unsplit   split
-//   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     737    37
-//   B 40, one of 131072, 39 of 1000,      1,     28/4           550    27
-//   B 200, one of 40000, 199 of 1000,     1,     32/8           244    76
-//   B 20, 33000 each,                     1,     32/8           211   147
-//   B 64, 33000 each,                     1,     32/8           379   388
-//   B 64, 33000 each,                     8,     28/4           401   415
-//   B 64, 1000 each, max_cached 131072,   1,     32/8            12    18   (what a loose bound costs)
-//   B 200, 1000 each, max_cached 131072,  1,     32/8            28    52
+//   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     771    57
+//   B 40, one of 131072, 39 of 1000,      1,     28/4           575    39
+//   B 200, one of 40000, 199 of 1000,     1,     32/8           294   114
+//   B 20, 33000 each,                     1,     28/4           223   132
+//   B 20, 33000 each,                     1,     32/8           251   260
+//   B 64, 33000 each,                     8,     28/4           580   595
+//   B 64, 1000 each, max_cached 131072,   1,     32/8            23    26   (what a loose bound costs)
 AttnSplit attn8_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh) {
   const Kind kind = kind_of(fp32, batch, G, hq, hkv, hd);
-  if (kind == Kind::WIDE) return AttnSplit{0, 0, batch, hd == 128 ? TILE : STEP};
+  if (kind == Kind::WIDE) return AttnSplit{0, 0, batch, TILE};
   const long ncol = (long)G * (hq / hkv), groups = hkv * (kind == Kind::COL1 ? (ncol + 15) / 16 : (ncol + 31) / 32);
   const long steps = ((long)max_cached + STEP - 1) / STEP + ((fresh ? G : 0) + STEP - 1) / STEP;
   AttnSplit s{0, 2 * NWAVE, batch, STEP};
-  // One round of what the CUs hold (four workgroups of one block each, two of the others): cutting
-  // B sequences by one length leaves up to B chunks more than that length divides out.
-  const long round = 256 * (kind == Kind::COL1 && !fp32 ? 4 : 2);
+  // As many workgroups as CUs, where that is a good many chunks to a sequence (B 16, 8000 keys, 1 row, 28/4 heads: 26 us, 28
+  // with four to a CU; B 4, 70001 to 131072: 64, 68).  Else one round of what the CUs hold: cutting B sequences by one
+  // length leaves up to B chunks more than that length divides out (the first of the table above: 71, 57).
+  const long round = 256 * (fp32 ? 3 : 256 / groups >= 4L * batch ? 1 : kind == Kind::COL1 ? 4 : 2);
   long target = round / groups - batch;
   const bool far = steps > 1024 && batch <= 256 && groups < round;
   if (far) target = std::max(target, (long)batch);
   // (the kernels count a batch's steps in 32 bits)
   if ((target <= batch && !far) || steps * batch > INT_MAX) return s;
   const long chunk = std::max((steps * batch + target - 1) / target, (long)s.chunk_min);
-  if (far || steps - std::max(chunk, steps * batch * groups / 160) > 56) {
+  const long busy = fp32 ? 256 : hd == 128 ? 90 : 123, cost = fp32 ? (hd == 128 ? 8 : 18) : hd == 128 ? 32 : 55;
+  if (far || steps - std::max(chunk, steps * batch * groups / busy) > cost) {
     s.target = (int)target;
     s.slots = (int)std::min(target + batch, batch * ((steps + s.chunk_min - 1) / s.chunk_min));
   }
