@@ -71,7 +71,7 @@ __global__ __launch_bounds__(NT) void pages_fork_kernel(PagesForkArgs a) {
 //            holders, the row copies it, unless it is the last of the holders and all of them write
 //   takes    a page for the copy, then want - have, from the ring's front
 //   gives    dropped pages without a holder left, by the last row that dropped them, behind the ring's end
-// Four launches, each of which needs all of the one before: clear the notes (a page's drops
+// Four launches (two of a small plan), each of which needs all of the one before: clear the notes (a page's drops
 // and writers, the last row of them), note, decide per row, then place everything by prefix sums over
 // the rows, which every workgroup of the last launch makes for itself.
 constexpr int WRITER = PAGES_MAX_ROWS;      // a writer's row in `last`: above every row that drops
@@ -106,9 +106,10 @@ __global__ __launch_bounds__(NT) void pages_clear_kernel(PagesPlanArgs a) {
   copy_ints(a.table_in, a.table_out, (long)a.batch * a.width, gid, gsz);
 }
 
-__global__ __launch_bounds__(NT) void pages_note_kernel(PagesPlanArgs a) {
+// by wave `w` of n
+__device__ __forceinline__ void note(const PagesPlanArgs& a, int w, int n) {
   const int lane = threadIdx.x & 63;
-  for (int b = blockIdx.x * (NT / 64) + (threadIdx.x >> 6); b < a.batch; b += gridDim.x * (NT / 64)) {
+  for (int b = w; b < a.batch; b += n) {
     const Lens l = lens_of(a, b);
     const int* row = a.table_in + (size_t)b * a.width;
     for (int j = l.want + lane; j < l.have; j += 64) {
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(NT) void pages_note_kernel(PagesPlanArgs a) {
 }
 
 // holders of page p after the drops
-__device__ __forceinline__ int holders(const PagesPlanArgs& a, int p) { return a.refs_out[p] - (a.todo[p] & 0xffff); }
+__device__ __forceinline__ int holders(const PagesPlanArgs& a, int p) { return a.refs_in[p] - (a.todo[p] & 0xffff); }
 
 // Whether row b, which drops page p, is the one that gives it back.  It leaves that as a note,
 // which only this row looks at: the counts change in the next launch.
@@ -138,9 +139,9 @@ __device__ __forceinline__ bool gives(const PagesPlanArgs& a, int b, int p) {
   return true;
 }
 
-__global__ __launch_bounds__(NT) void pages_decide_kernel(PagesPlanArgs a) {
+__device__ __forceinline__ void decide(const PagesPlanArgs& a, int w, int n) {
   const int lane = threadIdx.x & 63;
-  for (int b = blockIdx.x * (NT / 64) + (threadIdx.x >> 6); b < a.batch; b += gridDim.x * (NT / 64)) {
+  for (int b = w; b < a.batch; b += n) {
     const Lens l = lens_of(a, b);
     const int* row = a.table_in + (size_t)b * a.width;
     int given = 0;
@@ -159,6 +160,41 @@ __global__ __launch_bounds__(NT) void pages_decide_kernel(PagesPlanArgs a) {
       a.copies[b] = copies;
     }
   }
+}
+
+__global__ __launch_bounds__(NT) void pages_note_kernel(PagesPlanArgs a) {
+  note(a, blockIdx.x * (NT / 64) + (threadIdx.x >> 6), gridDim.x * (NT / 64));
+}
+__global__ __launch_bounds__(NT) void pages_decide_kernel(PagesPlanArgs a) {
+  decide(a, blockIdx.x * (NT / 64) + (threadIdx.x >> 6), gridDim.x * (NT / 64));
+}
+// A small plan's first three launches by one workgroup, a row to a wave, its notes in LDS until the last launch needs them (8 rows of
+// 4096 pages: the plan 9.3 us, with three launches for one 10.8; 64 rows of them 13.8 and 11.6).
+constexpr int PLAN_NT = 1024, PLAN_PAGES = 4096, PLAN_BATCH = PLAN_NT / 64;
+__global__ __launch_bounds__(PLAN_NT) void pages_small_kernel(PagesPlanArgs a) {
+  __shared__ int todo[PLAN_PAGES], last[PLAN_PAGES], bad;
+  const int tid = threadIdx.x;
+  PagesPlanArgs l = a;
+  l.todo = todo;
+  l.last = last;
+  l.bad = &bad;
+  for (int i = tid; i < a.n_pages; i += PLAN_NT) {
+    todo[i] = 0;
+    last[i] = -1;
+  }
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  note(l, tid >> 6, PLAN_NT / 64);
+  __syncthreads();
+  decide(l, tid >> 6, PLAN_NT / 64);
+  __syncthreads();
+  for (int i = tid; i < a.n_pages; i += PLAN_NT) {
+    a.todo[i] = todo[i];
+    a.last[i] = last[i];
+  }
+  if (tid == 0) *a.bad = bad;
+  copy_ints(a.refs_in, a.refs_out, a.n_pages, tid, PLAN_NT);
+  copy_ints(a.table_in, a.table_out, (long)a.batch * a.width, tid, PLAN_NT);
 }
 
 __device__ __forceinline__ long long scan64(long long v) {
@@ -297,7 +333,9 @@ __global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
 // Compaction.  U pages are in use.  Those from U on, in rising order, move to the free ones
 // below U, in rising order: there are as many of both.  The moves of a page are found by
 // prefix sums over the pages: a launch counts the pages in use of each block, and each
-// workgroup of the next one adds the blocks up for itself; a third one rewrites the tables.
+// workgroup of the next one adds the blocks up for itself (of up to COUNTED pages it counts them itself: 8192 pages 12.6 us,
+// 8193 in three launches 13.5); a third one rewrites the tables.
+constexpr int COUNTED = 4 * PAGES_BLOCK;
 __device__ __forceinline__ int block_sum_int(int v, int* red) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -328,15 +366,25 @@ __global__ __launch_bounds__(NT) void pages_moves_kernel(PagesCompactArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, nb = gridDim.x, me = blockIdx.x;
   // pages in use in all, before this block, and below U: blocks before U's, then its part of that block
   int all = 0, mine = 0, below = 0;
-  for (int i = tid; i < nb; i += NT) {
-    const int n = a.used[i];
-    all += n;
-    mine += i < me ? n : 0;
+  if (a.n_pages <= COUNTED) {
+#pragma unroll 8
+    for (int p = tid; p < a.n_pages; p += NT) {
+      const int n = a.refs_in[p] > 0;
+      all += n;
+      mine += p < me * PAGES_BLOCK ? n : 0;
+    }
+  } else {
+    for (int i = tid; i < nb; i += NT) {
+      const int n = a.used[i];
+      all += n;
+      mine += i < me ? n : 0;
+    }
   }
   const int U = block_sum_int(all, red);
   mine = block_sum_int(mine, red);
-  const int ub = U / PAGES_BLOCK;
+  const int ub = a.n_pages <= COUNTED ? 0 : U / PAGES_BLOCK;
   for (int i = tid; i < min(ub, nb); i += NT) below += a.used[i];
+#pragma unroll 8
   for (int p = ub * PAGES_BLOCK + tid; p < U; p += NT) below += a.refs_in[p] > 0;
   below = block_sum_int(below, red);
   const int moves = U - below;
@@ -433,16 +481,20 @@ void launch_pages_fork(const PagesForkArgs& a, hipStream_t st) {
 
 void launch_pages_plan(const PagesPlanArgs& a, hipStream_t st) {
   const long table = a.table_in == a.table_out ? 0 : (long)a.batch * a.width;
-  pages_clear_kernel<<<blocks(std::max((long)a.n_pages, table), 1024), NT, 0, st>>>(a);
-  pages_note_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
-  pages_decide_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
+  if (a.n_pages <= PLAN_PAGES && a.batch <= PLAN_BATCH && table <= 4 * PLAN_PAGES) {
+    pages_small_kernel<<<1, PLAN_NT, 0, st>>>(a);
+  } else {
+    pages_clear_kernel<<<blocks(std::max((long)a.n_pages, table), 1024), NT, 0, st>>>(a);
+    pages_note_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
+    pages_decide_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
+  }
   const long items = std::max((long)a.slot_rows, (long)a.batch * 64);
   pages_place_kernel<<<blocks(items, 512), NT, 3 * (a.batch + 1) * sizeof(int), st>>>(a);
 }
 
 void launch_pages_compact(const PagesCompactArgs& a, hipStream_t st) {
   const unsigned nb = (unsigned)(((long)a.n_pages + PAGES_BLOCK - 1) / PAGES_BLOCK);
-  pages_used_kernel<<<nb, NT, 0, st>>>(a);
+  if (a.n_pages > COUNTED) pages_used_kernel<<<nb, NT, 0, st>>>(a);
   pages_moves_kernel<<<nb, NT, 0, st>>>(a);
   pages_remap_kernel<<<blocks(std::max((long)a.batch * a.width, (long)a.n_pages / 2), 1024), NT, 0, st>>>(a);
 }
