@@ -249,3 +249,175 @@ def test_no_temperature_is_the_decision_of_archer_decide():
     z[:, 1023] = 99
     tok, logp = run(z, [0.5] * 16, dict(temperature=[0.0] * 16), exclude=1023)
     assert torch.equal(tok.long(), z[:, :1023].argmax(-1)) and not logp.any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kw", [dict(top_k=3500, top_p=0.95), dict(top_k=3999, top_p=0.5, min_p=0.001), dict(top_p=0.7), dict(top_k=3900), dict(min_p=0.3)])
+def test_long_lists_of_one_part(kw, dtype):
+    """A vocabulary that one workgroup has, most of which is kept."""
+    say(f"one part {kw} {dtype}")
+    rng = np.random.default_rng(11)
+    z = logits_of(rng, 3, 4000, 1.0, dtype, peaks=False)
+    check(z, rng.random(3), dict({k: [v] * 3 for k, v in kw.items()}, temperature=[1.0, 0.4, 3.0]), most_unsafe=0.4)
+
+
+@pytest.mark.parametrize("kw", [dict(top_p=0.4), dict(top_p=0.9), dict(top_k=30000), dict(top_k=60000, top_p=0.8), dict(top_k=100, top_p=0.5),
+                                dict(min_p=0.2), dict(min_p=0.5, top_p=0.99), {}])
+def test_values_that_many_tokens_share(kw):
+    """Two values of 50000 tokens each: lists that are too long.  Weights 1 and 1/4 (in 64 bits to 2^-52)."""
+    say(f"shared {kw}")
+    rng = np.random.default_rng(12)
+    z = torch.from_numpy(np.where(rng.random((2, 100000)) < 0.5, 0.0, -1.0)).float().cuda()
+    # 100 tokens of one weight and half of them: the border of top_p is the sum of the first 50 exactly, so every row is at one
+    at_border = kw.get("top_k") == 100
+    check(z, [0.3, 0.9], dict({k: [v] * 2 for k, v in kw.items()}, temperature=[1 / np.log(4.0)] * 2), most_unsafe=1.0 if at_border else 0.5)
+
+
+@pytest.mark.parametrize("kw", [dict(top_p=0.9), dict(top_k=20), dict(top_k=20, top_p=0.9), dict(min_p=0.1), {}])
+def test_the_first_tokens_say_little(kw):
+    """Rows that begin with thousands of masked tokens, or whose largest logits are hundreds of nats above the first ones."""
+    say(f"first tokens {kw}")
+    rng = np.random.default_rng(13)
+    z = logits_of(rng, 5, 30000, 2.0)
+    z[0, :4096] = -torch.inf
+    z[1, :12000] = -torch.inf
+    z[2] = -torch.inf
+    z[2, 29990:] = torch.arange(10).float() / 4
+    z[3, 20000:20050] += 300
+    z[4, 29999] += 5000
+    check(z, rng.random(5), {k: [v] * 5 for k, v in kw.items()}, most_unsafe=0.3)
+
+
+def test_more_rows_than_go_together():
+    rng = np.random.default_rng(14)
+    R = 2100
+    z = logits_of(rng, R, 260, 2.0)
+    kw = dict(temperature=rng.choice([0.0, 0.5, 1.0], R), top_k=rng.choice([0, 1, 20], R), top_p=rng.choice([0.5, 0.9, 1.0], R),
+              min_p=rng.choice([0.0, 0.02], R))
+    check(z, rng.random(R), {k: list(v) for k, v in kw.items()})
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+def test_rows_alone_are_the_same_bits(dtype):
+    """However a row is divided between workgroups."""
+    rng = np.random.default_rng(15)
+    R, V = 1024, 70000
+    z = torch.randn(R, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).to(T[dtype])
+    u = rng.random(R)
+    kw = dict(temperature=list(rng.choice([0.5, 1.0], R)), top_k=list(rng.choice([0, 40, 9000], R)),
+              top_p=list(rng.choice([0.6, 1.0], R)), min_p=list(rng.choice([0.0, 0.01], R)))
+    token, logp = run(z, u, kw)
+    for r in range(0, R, 41):
+        t, p = run(z[r:r + 1], u[r:r + 1], {k: v[r:r + 1] for k, v in kw.items()})
+        assert t.item() == token[r].item() and p.item() == logp[r].item(), r
+
+
+def test_two_calls_at_once_and_a_workspace_of_anything():
+    """Two streams, and the C call with a workspace whose bytes are not zeros, twice."""
+    rng = np.random.default_rng(16)
+    a = archer()
+    z = logits_of(rng, 64, 90000, 2.0)
+    u, p = dev_f32(rng.random(64)), dev_f32([0.9] * 64)
+    want = a.op_sample(z, u, top_p=p)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for s in streams * 3:
+        with torch.cuda.stream(s):
+            got.append(a.op_sample(z, u, top_p=p))
+    torch.cuda.synchronize()
+    for t, l in got:
+        assert torch.equal(t, want[0]) and torch.equal(l, want[1])
+    n = a.lib.archer_op_sample_ws_bytes(a.FP32, 64, 90000)
+    ws = torch.randint(0, 256, (n + 256,), dtype=torch.uint8, device="cuda")
+    guard = ws[n:].clone()
+    for _ in range(2):
+        token, logp = torch.zeros(64, dtype=torch.int32, device="cuda"), torch.zeros(64, device="cuda")
+        assert a.lib.archer_op_sample(a.FP32, 64, 90000, z.data_ptr(), z.stride(0), -1, u.data_ptr(), None, None, p.data_ptr(), None,
+                                      token.data_ptr(), logp.data_ptr(), ws.data_ptr(), n, a._raw_stream(torch.cuda.current_device())) == a.OK
+        assert torch.equal(token, want[0]) and torch.equal(logp, want[1])
+    assert torch.equal(ws[n:], guard)
+
+
+def test_samples_of_a_prompt_are_drawn():
+    """As they are used: four samples of one stored prompt; in each turn a token a sample is stored, attended from and the next
+    one drawn.  Eagerly against the oracle's draw from the same logits, then the turns again as replays of one graph."""
+    a = archer()
+    B, hq, hkv, hd, page, n_pages, width, turns = 4, 8, 2, 128, 32, 40, 8, 6
+    V, P = hq * hd, 70
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    tk, tv, tq, tl = rand(V, hkv, hd).half(), rand(V, hkv, hd).half(), rand(V, hq, hd).half(), rand(V, V) * 2
+    pk, pv = rand(hkv, P, hd).half(), rand(hkv, hd, P).half().transpose(1, 2)
+    u = torch.rand(turns, B, device="cuda", generator=g)
+    temp, top_p, top_k = dev_f32([1.0, 0.7, 1.0, 0.0]), dev_f32([0.9, 1.0, 0.8, 1.0]), dev_i32([0, 40, 100, 0])
+    cache = a.Cache8.empty(n_pages, page, hkv, hd)
+    ring, table = dev_i32(np.arange(n_pages)), dev_i32(np.full((B, width), -1))
+    pool, refs, lens, tok, draw = dev_i32([0, n_pages]), dev_i32([0] * n_pages), dev_i32([0] * B), dev_i32([0] * B), u[0].clone()
+
+    def begin():
+        ring.copy_(dev_i32(np.arange(n_pages)))
+        table.fill_(-1)
+        refs.zero_()
+        pool.copy_(dev_i32([0, n_pages]))
+        p = a.pages_plan(dev_i32([0] * B), dev_i32([P] + [0] * (B - 1)), page, table, ring, pool, refs, P, table_out=table, refs_out=refs)
+        pool.copy_(p.pool)
+        a.cache8_write(cache, table, dev_i32([0] * B), p.row_off, pk, pv)
+        _, st = a.pages_fork(dev_i32([0] * 3), dev_i32([1, 2, 3]), dev_i32([P] * 3), page, table, refs, refs_out=refs)
+        assert p.status.item() == 0 and st.item() == 0
+        lens.fill_(P)
+        tok.copy_(dev_i32([5, 5, 5, 6]))
+
+    def turn():
+        new = lens + 1
+        p = a.pages_plan(lens, new, page, table, ring, pool, refs, B, table_out=table, refs_out=refs)
+        a.pages_copy(cache.data, p.copy_src, p.copy_dst)
+        i = tok.long()
+        a.cache8_write(cache, table, lens, p.row_off, tk[i].transpose(0, 1).contiguous(), tv[i].transpose(0, 1).contiguous())
+        O = a.op_attention_cache8(tq[i].transpose(0, 1).contiguous(), cache, table, new, width * page)
+        logits = O.float() * 4 + tl[i]
+        t, lp = a.op_sample(logits, draw, temperature=temp, top_k=top_k, top_p=top_p, exclude=V - 1)
+        pool.copy_(p.pool)
+        lens.copy_(new)
+        tok.copy_(t)
+        return t, lp, logits, p.status
+
+    begin()
+    eager, unsafe = [], 0
+    for n in range(turns):
+        draw.copy_(u[n])
+        t, lp, logits, st = turn()
+        eager.append((t, lp, logits))
+        assert st.item() == 0
+        for b in range(B):
+            kw = dict(temperature=float(temp[b]), top_k=int(top_k[b]), top_p=float(top_p[b]), exclude=V - 1)
+            host, x = logits[b].cpu().numpy(), float(u[n, b])
+            want = osm.sample(host, x, **kw)
+            if not osm.safe(host, x, **kw):
+                unsafe += 1
+                continue
+            assert t[b].item() == want[0] and abs(lp[b].item() - want[1]) <= 2.0**-24 * abs(want[1]) + 2.0**-27
+    assert unsafe <= 1
+    # the samples' own pages: the shared ones are held by all
+    full = P // page
+    assert (refs[table[:, :full].long()] == B).all() and len(set(table[:, full].tolist())) == B
+    # and stored are the tokens that were drawn
+    k, _ = a.cache8_read(cache, (table[:, P // page] * page + P % page + 1).int())
+    want = tk[eager[0][0].long()].transpose(0, 1).float()
+    assert ((k.float() - want).abs() <= 2.0**-4 * want.abs() + 2.0**-9).all()      # (a scale of 1 at most: half a step of the subnormals)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    begin()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out = turn()
+    for again in range(2):
+        begin()
+        for n in range(turns):
+            draw.copy_(u[n])
+            graph.replay()
+            torch.cuda.synchronize()
+            assert out[3].item() == 0
+            for x, y in zip(out, eager[n]):
+                assert torch.equal(x, y), (again, n)
