@@ -12,7 +12,7 @@
 // the rounding, which is the hardware's own conversion.
 //
 // What bounds them: memory.  21500 rows of 32 heads of 128 in fp16, with pages of 64: the keys are stored in 60 us (4.4 TB/s of
-// rows and codes), the transposed values in 62, all are read back in 115 (4.6 TB/s).
+// rows and codes), the transposed values in 62, all are read back in 111 (4.8 TB/s).
 #include <algorithm>
 #include <climits>
 
@@ -143,6 +143,19 @@ __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, 
   auto token = [&](int e) __attribute__((always_inline)) { return KIND == 0 ? tid >> 3 : 8 * tb + (e & 7); };
   const int off = KIND == 0 ? (tid >> 3) * HD + dim
                             : L::voff(Tp) + tb * L::VBLK + (dim % (HD / 16)) / 2 * 256 + dim / (HD / 16) * 16;
+  // a block that is joined: its earlier tokens and their scale, before the barrier after which they are written
+  unsigned was[NB][EV / 4];
+  uint8_t *scale[NB], *dst[NB];
+#pragma unroll
+  for (int k = 0; k < NB; ++k) {
+    scale[k] = page[k] + L::soff(Tp) + (at[k] >> 5) * 2 + (KIND != 0);
+    dst[k] = page[k] + (size_t)at[k] * HD + off;      // (values: 32 tokens are 4 VBLK = 32 HD bytes as well)
+    old[k] = 0;
+    if (page[k] && v.unit * UNIT + k * C8_BLOCK < v.start) {
+      old[k] = *scale[k];
+      if (on) __builtin_memcpy(was[k], __builtin_assume_aligned(dst[k], EV), EV);
+    }
+  }
   __shared__ unsigned red[NB][NT / 64];
 #pragma unroll
   for (int k = 0; k < NB; ++k) {
@@ -165,23 +178,18 @@ __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, 
     unsigned m = 0;
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) m = max(m, red[k][i]);
-    uint8_t* scale = page[k] + L::soff(Tp) + (at[k] >> 5) * 2 + (KIND != 0);
-    uint8_t* dst = page[k] + (size_t)at[k] * HD + off;      // (values: 32 tokens are 4 VBLK = 32 HD bytes as well)
     unsigned eb = exponent_of(m);
-    if (p0 < v.start) {                   // joined: its earlier tokens, with their scale
-      old[k] = min(max((unsigned)*scale, (unsigned)C8_EMIN), (unsigned)C8_EMAX);
-      eb = max(eb, old[k]);
-      unsigned c[EV / 4];
-      if (on) __builtin_memcpy(c, __builtin_assume_aligned(dst, EV), EV);
+    if (p0 < v.start) {
+      const unsigned e = min(max(old[k], (unsigned)C8_EMIN), (unsigned)C8_EMAX);
+      eb = max(eb, e);
 #pragma unroll
-      for (int e = 0; e < EV; e += 4) {
+      for (int e4 = 0; e4 < EV; e4 += 4) {
         float y[4];
-        unpack4(y, on ? c[e / 4] : 0u, scale_of(old[k]));
+        unpack4(y, on ? was[k][e4 / 4] : 0u, scale_of(e));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (p0 + token(e + i) < v.start) x[k][e + i] = y[i];
+          if (p0 + token(e4 + i) < v.start) x[k][e4 + i] = y[i];
       }
-      __syncthreads();                    // (uniform) the scale is read before it is written
     }
     if (eb == (unsigned)C8_EMAX) {        // only here can an element lie beyond 448
       const float most = 448.f * scale_of(eb);
@@ -191,8 +199,8 @@ __device__ __forceinline__ void write_unit(const C8WriteArgs& a, const Span& v, 
     unsigned c[EV / 4];
 #pragma unroll
     for (int e = 0; e < EV; e += 4) c[e / 4] = pack4(&x[k][e], scale_of(eb));
-    if (on) __builtin_memcpy(__builtin_assume_aligned(dst, EV), c, EV);
-    if (tid == 0) *scale = (uint8_t)eb;
+    if (on) __builtin_memcpy(__builtin_assume_aligned(dst[k], EV), c, EV);
+    if (tid == 0) *scale[k] = (uint8_t)eb;
   }
 }
 
@@ -390,7 +398,7 @@ __global__ __launch_bounds__(LONG_UNIT * 4) void cache8_write_long_kernel(C8Writ
 //   keys    a thread 8 dimensions of a row
 //   values  8 rows of HD / 2 lanes, two dimensions each.  Where the slots follow each other in one page, the
 //           codes are those of two 8-token blocks at most, 16 bytes a lane each: shifted to begin at the first row,
-//           two dimensions' codes of a row side by side.  Else byte by byte (all of them: 165 us with the keys, not 115).
+//           two dimensions' codes of a row side by side.  Else byte by byte (all of them: 165 us with the keys, not 111).
 template <class T> __device__ __forceinline__ void put2(T* out, unsigned c, bool high, float sc) {      // (its low or high half)
   if constexpr (sizeof(T) == 2) {
     const f16x2 y = high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, sc, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, sc, false);
@@ -438,45 +446,62 @@ template <class T, int HD> __device__ __forceinline__ void read_values(const C8R
     }
     return;
   }
+  // every row's bytes are requested before the first is stored
+  unsigned y[8];
+  float sc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (r0 + i >= a.rows) break;
-    const int s = a.slots[r0 + i];
+    const int s = __shfl(slot, lane - p + i, 64);
     const bool ok = s >= 0 && s < all;
     const int t = ok ? s & (T_ - 1) : 0;
     const uint8_t* page = head(ok ? s : 0);
     const uint8_t* codes = page + L::voff(T_) + (t >> 3) * L::VBLK + off + (t & 7);
-    const unsigned y = codes[0] | (unsigned)codes[8] << 8;
-    const float sc = scale_of(page[L::soff(T_) + (t >> 5) * 2 + 1]);
-    put2(out + (size_t)i * HD, ok ? y : 0u, false, ok ? sc : 1.f);
+    y[i] = ok ? codes[0] | (unsigned)codes[8] << 8 : 0u;
+    sc[i] = scale_of(ok ? page[L::soff(T_) + (t >> 5) * 2 + 1] : 127u);
   }
-}
-template <class T, int HD> __device__ __forceinline__ void read_keys(const C8ReadArgs& a, long r, int u, int h) {
-  using L = C8<HD>;
-  if (r >= a.rows) return;
-  const int T_ = 1 << a.c.psh, slot = a.slots[r];
-  const bool ok = slot >= 0 && slot < (long)a.c.n_pages << a.c.psh;
-  const int s = ok ? slot : 0, t = s & (T_ - 1);
-  const uint8_t* page = a.c.data + ((size_t)(s >> a.c.psh) * a.c.hkv + h) * L::page_bytes(T_);
-  u32x2 c = *(const u32x2*)(page + (size_t)t * HD + u * 8);
-  const unsigned eb = page[L::soff(T_) + (t >> 5) * 2];
-  if (!ok) c[0] = c[1] = 0;
-  const float sc = scale_of(ok ? eb : 127u);
-  T* out = (T*)a.Ko + ((size_t)h * a.rows + r) * HD + u * 8;
-  if constexpr (sizeof(T) == 2) {
-    u32x4 y;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      y[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i], sc, false));
-      y[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i], sc, true));
+  for (int i = 0; i < 8; ++i)
+    if (r0 + i < a.rows) put2(out + (size_t)i * HD, y[i], false, sc[i]);
+}
+// rows r0, r0 + STEP, ...: all of them are requested before the first is stored
+template <class T, int HD, int N, int STEP> __device__ __forceinline__ void read_keys(const C8ReadArgs& a, long r0, int u, int h) {
+  using L = C8<HD>;
+  const int T_ = 1 << a.c.psh;
+  int slot[N];
+  u32x2 c[N];
+  float sc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) slot[i] = a.slots[min(r0 + i * STEP, (long)a.rows - 1)];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool ok = slot[i] >= 0 && slot[i] < (long)a.c.n_pages << a.c.psh;
+    const int s = ok ? slot[i] : 0, t = s & (T_ - 1);
+    const uint8_t* page = a.c.data + ((size_t)(s >> a.c.psh) * a.c.hkv + h) * L::page_bytes(T_);
+    c[i] = *(const u32x2*)(page + (size_t)t * HD + u * 8);
+    const unsigned eb = page[L::soff(T_) + (t >> 5) * 2];
+    if (!ok) c[i] = u32x2{0, 0};
+    sc[i] = scale_of(ok ? eb : 127u);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const long r = r0 + i * STEP;
+    if (r >= a.rows) break;
+    T* out = (T*)a.Ko + ((size_t)h * a.rows + r) * HD + u * 8;
+    if constexpr (sizeof(T) == 2) {
+      u32x4 y;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        y[2 * j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i][j], sc[i], false));
+        y[2 * j + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[i][j], sc[i], true));
+      }
+      *(u32x4*)out = y;
+    } else {
+      float y[8];
+      unpack4(y, c[i][0], sc[i]);
+      unpack4(y + 4, c[i][1], sc[i]);
+      *(f32x4*)out = f32x4{y[0], y[1], y[2], y[3]};
+      *(f32x4*)(out + 4) = f32x4{y[4], y[5], y[6], y[7]};
     }
-    *(u32x4*)out = y;
-  } else {
-    float y[8];
-    unpack4(y, c[0], sc);
-    unpack4(y + 4, c[1], sc);
-    *(f32x4*)out = f32x4{y[0], y[1], y[2], y[3]};
-    *(f32x4*)(out + 4) = f32x4{y[4], y[5], y[6], y[7]};
   }
 }
 constexpr int READ_ROWS = 64;      // rows of a workgroup
@@ -486,8 +511,7 @@ __global__ __launch_bounds__(NT) void cache8_read_kernel(C8ReadArgs a) {
   const long r0 = (long)blockIdx.x * READ_ROWS;
   const int h = blockIdx.y;
   if (blockIdx.z == 0) {
-#pragma unroll
-    for (int i = 0; i < READ_ROWS; i += NT / U) read_keys<T, HD>(a, r0 + i + threadIdx.x / U, threadIdx.x % U, h);
+    read_keys<T, HD, READ_ROWS * U / NT, NT / U>(a, r0 + threadIdx.x / U, threadIdx.x % U, h);
   } else {
 #pragma unroll
     for (int i = 0; i < READ_ROWS; i += V * W) read_values<T, HD>(a, r0 + i + (threadIdx.x >> 6) * V, h);
