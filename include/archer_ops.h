@@ -5,8 +5,9 @@
  * decoding path exactly as the model path launches it (same kernels, same tile and split
  * choices for the same shapes), on caller-provided device buffers.  They exist so that the
  * kernels can be checked element by element at full model sizes and timed in
- * isolation.  The 4-bit paged prompt cache's calls are operators of their own, for
- * programs that hold prompts in it: the decoding path keeps its fp16 cache and
+ * isolation.  The calls of the 4-bit and 8-bit paged prompt caches, of pages that sequences
+ * share and of sampling are operators of their own, for programs that hold prompts
+ * so and draw tokens: the decoding path keeps its fp16 cache and its greedy decision and
  * runs none of them.  Conventions as in archer.h: device pointers, caller-owned
  * memory, asynchronous on the given stream, host-side argument checks.
  */
