@@ -71,7 +71,7 @@ __global__ __launch_bounds__(NT) void pages_fork_kernel(PagesForkArgs a) {
 //            holders, the row copies it, unless it is the last of the holders and all of them write
 //   takes    a page for the copy, then want - have, from the ring's front
 //   gives    dropped pages without a holder left, by the last row that dropped them, behind the ring's end
-// Four launches (two of a small plan), each of which needs all of the one before: clear the notes (a page's drops
+// Four launches (one of a small plan), each of which needs all of the one before: clear the notes (a page's drops
 // and writers, the last row of them), note, decide per row, then place everything by prefix sums over
 // the rows, which every workgroup of the last launch makes for itself.
 constexpr int WRITER = PAGES_MAX_ROWS;      // a writer's row in `last`: above every row that drops
@@ -168,35 +168,6 @@ __global__ __launch_bounds__(NT) void pages_note_kernel(PagesPlanArgs a) {
 __global__ __launch_bounds__(NT) void pages_decide_kernel(PagesPlanArgs a) {
   decide(a, blockIdx.x * (NT / 64) + (threadIdx.x >> 6), gridDim.x * (NT / 64));
 }
-// A small plan's first three launches by one workgroup, a row to a wave, its notes in LDS until the last launch needs them (8 rows of
-// 4096 pages: the plan 9.3 us, with three launches for one 10.8; 64 rows of them 13.8 and 11.6).
-constexpr int PLAN_NT = 1024, PLAN_PAGES = 4096, PLAN_BATCH = PLAN_NT / 64;
-__global__ __launch_bounds__(PLAN_NT) void pages_small_kernel(PagesPlanArgs a) {
-  __shared__ int todo[PLAN_PAGES], last[PLAN_PAGES], bad;
-  const int tid = threadIdx.x;
-  PagesPlanArgs l = a;
-  l.todo = todo;
-  l.last = last;
-  l.bad = &bad;
-  for (int i = tid; i < a.n_pages; i += PLAN_NT) {
-    todo[i] = 0;
-    last[i] = -1;
-  }
-  if (tid == 0) bad = 0;
-  __syncthreads();
-  note(l, tid >> 6, PLAN_NT / 64);
-  __syncthreads();
-  decide(l, tid >> 6, PLAN_NT / 64);
-  __syncthreads();
-  for (int i = tid; i < a.n_pages; i += PLAN_NT) {
-    a.todo[i] = todo[i];
-    a.last[i] = last[i];
-  }
-  if (tid == 0) *a.bad = bad;
-  copy_ints(a.refs_in, a.refs_out, a.n_pages, tid, PLAN_NT);
-  copy_ints(a.table_in, a.table_out, (long)a.batch * a.width, tid, PLAN_NT);
-}
-
 __device__ __forceinline__ long long scan64(long long v) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -217,15 +188,15 @@ __device__ __forceinline__ int find_row(const int* off, int n, int v) {
   return lo;
 }
 
-__global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
-  extern __shared__ int sh[];
+// sh: 3 (B + 1) ints of LDS; by workgroup `me` of n, of N threads
+template <int N> __device__ __forceinline__ void place(const PagesPlanArgs& a, int* sh, int me, int n) {
   const int B = a.batch, tid = threadIdx.x, lane = tid & 63, T = 1 << a.psh;
   int *taken = sh, *given = sh + (B + 1), *rows = sh + 2 * (B + 1);    // exclusive sums
-  __shared__ long long part[3][NT / 64];
+  __shared__ long long part[3][N / 64];
   __shared__ int bad_len;
   if (tid == 0) bad_len = 0;
   __syncthreads();
-  const int per = (B + NT - 1) / NT, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+  const int per = (B + N - 1) / N, b0 = min(B, tid * per), b1 = min(B, b0 + per);
   long long st = 0, sg = 0, sr = 0;
   for (int b = b0; b < b1; ++b) {
     const Lens l = lens_of(a, b);
@@ -240,7 +211,7 @@ __global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
   __syncthreads();
   long long bt = it - st, bg = ig - sg, br = ir - sr, tt = 0, tg = 0, tr = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) {
+  for (int i = 0; i < N / 64; ++i) {
     if (i < w) { bt += part[0][i]; bg += part[1][i]; br += part[2][i]; }
     tt += part[0][i]; tg += part[1][i]; tr += part[2][i];
   }
@@ -270,7 +241,7 @@ __global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
     const unsigned k = (unsigned)head + (unsigned)i, n = (unsigned)a.n_pages;
     return k >= n ? k - n : k;
   };
-  const int gid = blockIdx.x * NT + tid, gsz = gridDim.x * NT;
+  const int gid = me * N + tid, gsz = n * N;
   if (gid == 0) {
     *a.status = status;
     a.pool_out[0] = status ? head : (int)ring((int)tt);
@@ -327,6 +298,33 @@ __global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
     }
     a.slots[r] = s;
   }
+}
+__global__ __launch_bounds__(NT) void pages_place_kernel(PagesPlanArgs a) {
+  extern __shared__ int sh[];
+  place<NT>(a, sh, blockIdx.x, gridDim.x);
+}
+// A small plan by one workgroup, a row to a wave, its notes in LDS (16 rows of 4096 pages: 8.9 us, in four
+// launches 11.5; 8 rows that take 16384 slots 9.4 and 10.4).
+constexpr int PLAN_NT = 1024, PLAN_PAGES = 4096, PLAN_BATCH = PLAN_NT / 64, PLAN_SLOTS = 16384;
+__global__ __launch_bounds__(PLAN_NT) void pages_small_kernel(PagesPlanArgs a) {
+  __shared__ int todo[PLAN_PAGES], last[PLAN_PAGES], sums[3 * (PLAN_BATCH + 1)], bad;
+  const int tid = threadIdx.x;
+  a.todo = todo;
+  a.last = last;
+  a.bad = &bad;
+  for (int i = tid; i < a.n_pages; i += PLAN_NT) {
+    todo[i] = 0;
+    last[i] = -1;
+  }
+  if (tid == 0) bad = 0;
+  copy_ints(a.refs_in, a.refs_out, a.n_pages, tid, PLAN_NT);
+  copy_ints(a.table_in, a.table_out, (long)a.batch * a.width, tid, PLAN_NT);
+  __syncthreads();
+  note(a, tid >> 6, PLAN_NT / 64);
+  __syncthreads();
+  decide(a, tid >> 6, PLAN_NT / 64);
+  __syncthreads();
+  place<PLAN_NT>(a, sums, 0, 1);
 }
 
 // ---------------------------------------------------------------------------
@@ -481,13 +479,13 @@ void launch_pages_fork(const PagesForkArgs& a, hipStream_t st) {
 
 void launch_pages_plan(const PagesPlanArgs& a, hipStream_t st) {
   const long table = a.table_in == a.table_out ? 0 : (long)a.batch * a.width;
-  if (a.n_pages <= PLAN_PAGES && a.batch <= PLAN_BATCH && table <= 4 * PLAN_PAGES) {
+  if (a.n_pages <= PLAN_PAGES && a.batch <= PLAN_BATCH && table <= 4 * PLAN_PAGES && a.slot_rows <= PLAN_SLOTS) {
     pages_small_kernel<<<1, PLAN_NT, 0, st>>>(a);
-  } else {
-    pages_clear_kernel<<<blocks(std::max((long)a.n_pages, table), 1024), NT, 0, st>>>(a);
-    pages_note_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
-    pages_decide_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
+    return;
   }
+  pages_clear_kernel<<<blocks(std::max((long)a.n_pages, table), 1024), NT, 0, st>>>(a);
+  pages_note_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
+  pages_decide_kernel<<<blocks((long)a.batch * 64, 1024), NT, 0, st>>>(a);
   const long items = std::max((long)a.slot_rows, (long)a.batch * 64);
   pages_place_kernel<<<blocks(items, 512), NT, 3 * (a.batch + 1) * sizeof(int), st>>>(a);
 }

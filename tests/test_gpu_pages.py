@@ -168,3 +168,17 @@ def test_copy_into_far_pages():
     data[69, 0, -5:] = 9
     a.pages_copy(data, dev_i32([3, 69]), dev_i32([66, 1]))
     assert (data[66] == 7).all() and (data[1, 0, -5:] == 9).all() and not data[1, 0, :-5].any() and not data[67].any()
+
+
+@pytest.mark.parametrize("B,n_pages,width,slots", [(16, 4096, 12, 0), (17, 4096, 12, 0), (16, 4097, 12, 0), (16, 4096, 1024, 0), (16, 4096, 1025, 0),
+                                                   (15, 4000, 12, 16384), (15, 4000, 12, 16385)])
+def test_plans_at_the_end_of_small_ones(B, n_pages, width, slots):
+    """The largest plan that one workgroup makes and the first ones that it does not: rows, pages, table entries, slots."""
+    say(f"small plan B={B} pages={n_pages} width={width} slots={slots}")
+    old, new, page, table, ring, pool, refs, rows = _large(B, 32, n_pages, B + width, 3)
+    table = np.pad(table, ((0, 0), (0, width - table.shape[1])), constant_values=-1)
+    args = old, new, page, table, ring, pool, refs, max(rows, slots)
+    want = op.plan(*args)
+    assert want[8] == 0 and (want[6] >= 0).any()
+    gpu_call("plan", args, want, False)
+    gpu_call("plan", args, want, True)
