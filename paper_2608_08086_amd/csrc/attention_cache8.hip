@@ -31,6 +31,7 @@ __device__ __forceinline__ void expand8(Frag<float>& f, unsigned lo, unsigned hi
 __device__ __forceinline__ float scale_of(unsigned eb) { return __uint_as_float(eb << 23); }
 
 // a piece's codes of the first m of its 8 keys; zeros after them, for a code there may be a NaN
+// (a block without any key may never have been stored: its scale is taken as 1, for zeros times an infinite one are NaNs)
 __device__ __forceinline__ u32x4 first_keys(u32x4 v, int m) {
   const unsigned lo = m >= 4 ? ~0u : m <= 0 ? 0u : (1u << (8 * m)) - 1;
   const unsigned hi = m >= 8 ? ~0u : m <= 4 ? 0u : (1u << (8 * m - 32)) - 1;
@@ -80,7 +81,7 @@ template <int HD> struct Fmt8 {
     }
   }
   template <class T, class V> __device__ __forceinline__ static void values(Raw& raw, int valid, int lg, V&& value) {
-    const float sc = scale_of(raw.vs);
+    const float sc = scale_of(valid > 0 ? raw.vs : 127u);
     if (valid < STEP) {
       const int m = valid - 8 * local_value(lg);
 #pragma unroll
@@ -124,7 +125,7 @@ template <int HD> struct Fmt8 {
       const int valid = (val >> (16 * vhalf)) & 0xffff;
       u32x4 v = r.v;
       if (valid < 32) v = first_keys(v, valid - 8 * local_value(lane >> 4));
-      const float ks = scale_of(r.sc & 255u), vs = scale_of(r.sc >> 8);
+      const float ks = scale_of(r.sc & 255u), vs = scale_of(valid > 0 ? r.sc >> 8 : 127u);
       Frag<f16> a, b, c, d;
       expand8(a, r.k[0], r.k[1], ks);
       expand8(b, r.k[2], r.k[3], ks);
