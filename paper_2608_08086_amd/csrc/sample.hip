@@ -431,6 +431,7 @@ struct Cut {
   unsigned key;
   int last;
 };
+INLINE Cut everything() { return Cut{KEY_LOWEST + 1, INT_MAX}; }      // (the lowest finite value's tokens among it)
 
 // clears the parts of the keys lo .. hi; how far a key's distance from lo is shifted to be its part
 template <int NT> INLINE int clear_parts(unsigned lo, unsigned hi) {
@@ -1106,7 +1107,7 @@ template <class T> __global__ __launch_bounds__(DECIDE_NT) void sample_finish(Ca
     finish_list<NT>(c.a, v, q, o.k, o.by_p || (o.k && w.by_p), w.p, o.floor_l, o.total, o.best, o.bin, w.u, r);
     return;
   }
-  Cut cut{KEY_LOWEST, -1};               // everything
+  Cut cut = everything();
   if (o.mode == CUT && o.bin >= 0) {
     const double unit = list_weights<NT>(v, q, s.edge[o.bin] * 1.04);      // (no token of the bin weighs more: e^(1/32))
     unsigned long long last = ~0ull;
@@ -1139,7 +1140,7 @@ template <class T> INLINE void whole(const Call& c, int at) {
   v.inf = inf;
   v.share = ((v.V + NW - 1) / NW + 255) / 256 * 256;
   load_edges<NT>(c);
-  Cut cut{KEY_LOWEST, -1};               // everything
+  Cut cut = everything();
   const bool masses = w.by_p || (w.by_m && !w.by_k);
   double total = 0;
 #pragma unroll 1
