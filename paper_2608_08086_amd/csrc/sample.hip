@@ -337,6 +337,8 @@ template <class T> INLINE unsigned long long first_token(const View<T>& v, int i
 // ---- the second pass
 // The wave's tokens [i0, i1) of bin b, or with ALL those of every bin from b on, to put(~key, index).  Without ALL the
 // weights of the pieces' higher bins go into seg.  Pieces whose maximum (tops) is lower are not read: 64 of them at most.
+// (A logit below `low` is raised to it for a place that is finite.  At temperatures from 1e37 on, where `low` ends at the
+// lowest float, that place may be in bin b or above it: so the logit is looked at, too.)
 template <bool ALL, int NT, class T, class F> INLINE void collect(const View<T>& v, int b, int i0, int i1, Keys tops, Doubles seg, F&& put) {
   auto& s = lds<NT>();
   const int lane = lane_id(), mine = i0 + lane * PIECE;
@@ -354,11 +356,11 @@ template <bool ALL, int NT, class T, class F> INLINE void collect(const View<T>&
 #pragma unroll
       for (int e = 0; e < M; ++e) p[e] = v.place(at_least(l[e], low));
 #pragma unroll
-      for (int e = 0; e < M; ++e) x += s.edge[p[e].bin > b ? p[e].bin : BINS] * series(p[e].x, 1.0);
+      for (int e = 0; e < M; ++e) x += s.edge[(p[e].bin > b) & (l[e] >= low) ? p[e].bin : BINS] * series(p[e].x, 1.0);
     }
 #pragma unroll
     for (int e = 0; e < M; ++e) {
-      if (ALL ? l[e] >= low : p[e].bin == b && b >= 0) {
+      if (l[e] >= low && (ALL || (p[e].bin == b && b >= 0))) {
         if (ALL && v.place(l[e]).bin < b) continue;
         put((unsigned long long)~key_of(l[e]) << 32 | (unsigned)index(e));
       }
