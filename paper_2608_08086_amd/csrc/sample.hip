@@ -390,12 +390,16 @@ INLINE void write(const SampleArgs& a, int r, int token, float logp) {
 }
 
 // ---- cuts
-// The bin, from the highest on, in which the sum over the bins reaches `target` (strict: exceeds it), and the sum above
+// The bin, from the highest on, at whose end the sum over the bins reaches `target` (strict: exceeds it), and the sum above
 // it; -1 where it does not.  The sum is that of the counts (unit 0), of the masses in `unit`, or (unit < 0) in those of
-// the bins' edges.
+// the bins' edges.  A wave's or thread's end and the next one's start are sums of other groupings and may differ in their last
+// bits.  So the crossing is in the first wave of any weight whose end reaches the target, and there at the first such thread, then
+// bin, or the last one of any weight if the end is reached at none: one thread's, whatever the rounding.
 template <int NT> INLINE int cross(double target, double unit, double& above, bool strict = false) {
   constexpr int E = BINS / NT;
   auto& s = lds<NT>();
+  const int lane = lane_id(), w = wave_id();
+  auto reached = [&](double y) { return strict ? y > target : y >= target; };
   double x[E], t = 0;
   __syncthreads();
 #pragma unroll
@@ -404,16 +408,30 @@ template <int NT> INLINE int cross(double target, double unit, double& above, bo
     x[e] = unit == 0 ? (double)s.count[b] : (double)s.mass[b] * (unit < 0 ? s.edge[b] * (1 / UNIT) : unit);
     t += x[e];
   }
-  double all, y = scan_all<NT>(t, all) - t;
-  if (threadIdx.x == 0) s.flag = -1;
+  const double upto = wave_scan64(t);
+  if (lane == 63) s.redd[w] = upto;
   __syncthreads();
+  const double wave = lane < NT / 64 ? s.redd[lane] : 0.0, ends = wave_scan64(wave);
+  const unsigned long long waves = __ballot(wave > 0 && reached(ends));
+  if (waves ? w == __ffsll(waves) - 1 : w == 0) {
+    double y = upto + (w ? lane_value(ends, w - 1) : 0.0);
+    const unsigned long long any = __ballot(t > 0), hit = __ballot(t > 0 && reached(y));
+    if (lane == (hit ? __ffsll(hit) - 1 : any ? 63 - __clzll((long long)any) : 0)) {
+      y -= t;
+      double cut = y;
+      int at = 0;
+      bool open = true;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if (strict ? y <= target && y + x[e] > target : y < target && y + x[e] >= target) {
-      s.flag = BINS - 1 - (threadIdx.x * E + e);
-      s.cut = y;
+      for (int e = 0; e < E; ++e) {
+        const bool here = open && x[e] > 0;
+        at = here ? e : at;
+        cut = here ? y : cut;
+        y += x[e];
+        open = open && !(here && reached(y));
+      }
+      s.cut = cut;
+      s.flag = waves ? BINS - 1 - (threadIdx.x * E + at) : -1;
     }
-    y += x[e];
   }
   __syncthreads();
   above = s.cut;
@@ -1032,7 +1050,7 @@ template <class T> __global__ __launch_bounds__(DECIDE_NT) void sample_decide(Ca
     }
     return;
   }
-  if (v.place(best).bin >= BINS || v.m0 > (double)best) {      // (m0 above it: there are infinite ones alone)
+  if (v.place(best).bin >= BINS) {      // (an infinite one, too)
     if (tid == 0) {
       leave_whole(c.s, i);
       c.s.row[i].mode = DONE;

@@ -1,12 +1,15 @@
-"""GPU parity of sampling where a rule meets the ends of a type: rows of the lowest finite value, temperatures at which
-every finite logit weighs the same, filters that cut nothing.  Tolerances as in ``test_gpu_sample``."""
+"""GPU parity of sampling where a rule meets the ends of a type or of its own sums: rows of the lowest finite value,
+temperatures at which every finite logit weighs the same, filters that cut nothing, and a top_p whose border lies
+between two partial sums.  Tolerances as in ``test_gpu_sample``."""
+
+import math
 
 import numpy as np
 import pytest
 import torch
 
 from gpu_util import say
-from test_gpu_sample import T, check
+from test_gpu_sample import T, check, run
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +75,36 @@ def test_cuts_among_masked_tokens_at_large_temperatures(kw):
     z[4:] = -torch.inf
     z[4:, 7::13] = 1.5
     check(z, rng.random(n), dict({k: [v] * n for k, v in kw.items()}, temperature=[np.inf, 1e38] * 4), exclude=1, most_unsafe=0.3)
+
+
+# -- a border between two partial sums --------------------------------------------------------------
+def _row_at_a_border(rng, over):
+    """A token of weight 1, and others of 2^15 - 1 + `over` together, each of about e^(-1/16) and by themselves."""
+    total = 2.0**15 - 1 + over
+    l = rng.uniform(-0.075, -0.069, 35300).astype(np.float32)
+    w = np.cumsum(np.exp(l.astype(np.float64)))
+    l = l[:int(np.searchsorted(w, total - 0.93)) + 1]
+    # what lacks is shared out among 3000 of them, and one takes what is left: its logits are 2^-27 apart
+    share = l[:3000].astype(np.float64)
+    l[:3000] = share + np.log1p((total - 0.93 - w[len(l) - 1]) / np.exp(share).sum())
+    last = total - math.fsum(np.exp(l.astype(np.float64)))
+    l = np.append(l, np.float32(math.log(last)))
+    assert abs(math.fsum(np.exp(l.astype(np.float64))) - total) < over / 2
+    return np.concatenate([[np.float32(0)], l])
+
+
+def test_top_p_at_a_border_between_two_partial_sums():
+    """A first token of weight 1, the others with 2^15 - 1 and 2^-24 more: top_p = 2^-15 asks for the first one and a little
+    more than none of the next.  The sum up to the second one and that without it lie 2^-38 apart in 64 bits, which may
+    be more than the border is from either: one token is kept or two, whichever rounding, never all of them."""
+    rng = np.random.default_rng(11)
+    rows = [_row_at_a_border(rng, 2.0**-24) for _ in range(32)]
+    V = max(len(r) for r in rows)
+    z = np.full((len(rows), V), -np.inf, np.float32)
+    for i, r in enumerate(rows):
+        z[i, :len(r)] = r
+    tok, logp = (x.cpu().numpy() for x in run(torch.from_numpy(z).cuda(), [0.75] * len(rows), dict(top_p=[2.0**-15] * len(rows))))
+    for i, row in enumerate(z):
+        order = np.argsort(-row, kind="stable")
+        assert tok[i] in order[:2], (i, tok[i], order[:2])
+        assert logp[i] >= math.log(0.25)
