@@ -77,6 +77,21 @@ def test_cuts_among_masked_tokens_at_large_temperatures(kw):
     check(z, rng.random(n), dict({k: [v] * n for k, v in kw.items()}, temperature=[np.inf, 1e38] * 4), exclude=1, most_unsafe=0.3)
 
 
+# -- top_k and top_p together where one value is there too often ------------------------------------
+@pytest.mark.parametrize("k,p,n", [(100, 0.505, 51), (101, 0.5, 51), (100, 0.995, 100), (7, 0.01, 1)])
+def test_top_p_of_top_k_in_a_value_that_many_tokens_share(k, p, n):
+    """p of the k tokens' weight lies half a token from a border: n tokens are left, the first ones."""
+    say(f"shared k={k} p={p}")
+    rng = np.random.default_rng(5)
+    rows = 24
+    z = torch.from_numpy(np.where(rng.random((rows, 60000)) < 0.5, 0.0, -1.0)).float().cuda()
+    u = (np.arange(rows) + 0.31) / rows
+    tok = check(z, u, dict(top_k=[k] * rows, top_p=[p] * rows, temperature=[1 / math.log(4.0)] * rows), most_unsafe=0.0)
+    for r in range(rows):
+        first = np.flatnonzero(z[r].cpu().numpy() == 0)
+        assert tok[r] == first[int(u[r] * n)]
+
+
 # -- a border between two partial sums --------------------------------------------------------------
 def _row_at_a_border(rng, over):
     """A token of weight 1, and others of 2^15 - 1 + `over` together, each of about e^(-1/16) and by themselves."""
