@@ -227,7 +227,8 @@ size_t archer_cache8_bytes(const archer_cache8 *cache);
  * to [-15, 7]; elements are rounded to the nearest e4m3 value of x / 2^e, ties to the even code, and
  * saturate at 448 * 2^e (57344 at most).  Where a block holds earlier tokens of the sequence e
  * is no less than theirs, and they are rounded once more in the new scale (exact but for elements
- * below 2^-14 of the block's largest).  Every stored element is exact in fp16.  A NaN stays one. */
+ * below 2^-6 * 2^e, less than 2^-13 of the block's largest).  Every stored element is exact in fp16.
+ * A NaN stays one. */
 archer_status archer_cache8_write(int32_t dtype, const archer_cache8 *cache, int32_t batch, const int32_t *table,
                                   int32_t max_pages, const int32_t *start, const int32_t *row_off, int32_t rows,
                                   const void *K, int64_t k_head, int64_t k_row, const void *V, int64_t v_head,
@@ -238,7 +239,8 @@ archer_status archer_cache8_read(int32_t dtype, const archer_cache8 *cache, int3
                                  const int32_t *slot_map, void *K, void *V, void *hip_stream);
 
 /* archer_op_attention_cache4 over the 8-bit cache: the same arguments, limits and results of rows
- * without keys.  fp16: probabilities are rounded to fp16, and nothing else is but the output. */
+ * without keys.  What blocks without a token of the sequence hold does not matter.  fp16:
+ * probabilities are rounded to fp16, and nothing else is but the output. */
 size_t archer_op_attention_cache8_ws_bytes(int32_t dtype, int32_t batch, int32_t G, int32_t Hq, int32_t Hkv,
                                            int32_t hd, int32_t max_cached, int32_t fresh);
 archer_status archer_op_attention_cache8(int32_t dtype, const archer_cache8 *cache, int32_t batch, int32_t G,
@@ -334,12 +336,15 @@ archer_status archer_pages_copy(int64_t page_bytes, int32_t n_pages, int32_t n_p
  * kept are the tokens of S2 that are in S3, and the first token of the order always; the token
  * drawn is the first one by index at which the sum of the kept weights up to it exceeds u times all of
  * it (with rounding at u near 1: the last one of any weight).  A temperature that is not
- * positive takes the first token of the order, with logp 0.  Weights are summed in 64 bits, by fixed
- * orders: a row's result does not depend on the other rows or on the run.  Infinite logits share
- * the weight; -infinity has none.  A row without a token (all -infinity or excluded): token -1, logp
+ * positive takes the first token of the order, with logp 0.  Weights are off by 2^-44 of themselves or
+ * 2^-49 of the largest one at most and summed in 64 bits, by fixed orders: a row's result does not depend
+ * on the other rows or on the run, but a sum as near as that to a border may fall on either side of it.  A
+ * token whose z is more than 33 below the largest may count as one without weight (2^19 of them
+ * together: 2^-28.6 of the row's).  Infinite logits share the weight; -infinity has none, every finite
+ * value has one, the lowest too.  A row without a token (all -infinity or excluded): token -1, logp
  * -infinity; a row with a NaN: token -1, logp NaN.
- *   workspace  device scratch of archer_op_sample_ws_bytes bytes (0 for a bad shape), 256-byte aligned;
- *              nothing in it is kept for another call */
+ *   workspace  device scratch of archer_op_sample_ws_bytes bytes (0 for a bad shape; 0.3 MB a row, of 1024 rows
+ *              at most), 256-byte aligned; nothing in it is kept for another call */
 size_t archer_op_sample_ws_bytes(int32_t dtype, int32_t rows, int32_t vocab);
 archer_status archer_op_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t row_stride,
                                int32_t exclude, const float *u, const float *temperature, const int32_t *top_k,

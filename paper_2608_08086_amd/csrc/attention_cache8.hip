@@ -151,17 +151,18 @@ template <int HD> struct Fmt8 {
 // fresh keys, heads of 128 dimensions, unless said otherwise):
 //   COL1: up to 16 columns of a key head, a block to a workgroup.
 //   COL2: more of them.  Against one block, it expands a step for 32 columns: B 32, 2000 + 8
-//     keys, 8 rows, 28/4 heads: 24.1, one block 25.7.
+//     keys, 8 rows, 28/4 heads: 25.2, one block 27.9.
 //   WIDE: columns enough that the row kernel's workgroups of 256 occupy half of the CUs:
-//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   114   COL2 198
-//       B 16, 1000 + 128,      128,      16/16          34         38
-//       B  8, 1000 + 128,      128,      32/32          35         39
-//       B  4, 512 + 256,       256,      32/32          31         37
-//       B  4, 1000 + 192,      192,      32/32          42         34    (so not here)
-//       B  2, 4096 + 256,      256,      32/32         116         53    (nor here)
-//       B  8, 1000 + 96,       96,       32/32          34         30    (nor here)
-//     With 64 dimensions four blocks of columns a wave take longer than two (B 16, 1344 + 256 keys,
-//     256 rows, 32/32 heads: 111, two 79), whatever the batch.
+//       B 16, 1344 + 256 keys, 256 rows, 32/32 heads   125   COL2 206
+//       B 16, 1000 + 128,      128,      16/16          35         39
+//       B  8, 1000 + 128,      128,      32/32          38         43
+//       B  4, 512 + 256,       256,      32/32          32         38
+//       B  4, 1000 + 192,      192,      32/32          43         35    (so not here)
+//       B  2, 4096 + 256,      256,      32/32         120         57    (nor here)
+//       B  8, 1000 + 96,       96,       32/32          35         32    (nor here)
+//     With 64 dimensions always two blocks of columns.  Four to a wave, each with its own, are faster only where
+//     they make two workgroups for every CU: 256 rows, 32/32 heads, B 16, 1344 + 256 keys 90, four 77; B 8,
+//     4096 + 256 107, four 132; B 8, 1344 + 256 51, four 56; 128 rows, B 16, 1000 + 128 40, four 54.
 enum class Kind { COL1, COL2, WIDE };
 Kind kind_of(int fp32, int batch, int G, int hq, int hkv, int hd) {
   const long ncol = (long)G * (hq / hkv), all = ncol * batch * hkv;
@@ -179,7 +180,7 @@ void launch_kind(PagedAttnArgs a, hipStream_t st) {
   const long ncol = (long)a.G * (a.hq / a.hkv), cols = kind == Kind::COL1 ? 16 : kind == Kind::COL2 ? 32 : 256;
   const dim3 grid((unsigned)(a.hkv * ((ncol + cols - 1) / cols)), (unsigned)a.slots);
   // More workgroups than CUs: the longest sequences first, or the last ones to start are waited
-  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 106 us, not 126).  In the
+  // for (16 sequences of 681 to 1971 cached and 256 fresh keys, 32 heads: 125 us, not 140).  In the
   // column kernel, several to a CU and shorter, it gives nothing (64 of 512 + 32 keys, 32 rows, 32 heads: 73 us, 72).
   a.sorted = kind == Kind::WIDE && a.batch > 1 && (long)grid.x * a.batch > 256;
   if (kind == Kind::COL1) {
@@ -207,12 +208,12 @@ void launch_kind(PagedAttnArgs a, hipStream_t st) {
 // gives, in fp32 it takes all of the CUs.  Cutting the sequences costs the merge's launch and a second pass over the
 // queries, about 5 us.  So it has to save more steps than that is.  Unsplit and split, one row of 28/4 heads:
 //                      128 dimensions   64           fp32
-//   B  1,  1000 keys    8.4   10.1       6.2    9.2   23.5   14.1
-//   B  1,  2000        12.8   10.1       9.3    9.4   43.0   14.1
-//   B  4,  4000        21.6   10.7      15.1    9.8   81.4   14.4
-//   B 16,  2000        13.3   12.8       9.5   11.1   43.4   19.5
-//   B 16,  4000        22.1   17.7      15.7   13.4   82.1   30.6
-//   B 32,  2000        14.1   17.5       9.9   13.3   43.2   33.2
+//   B  1,  1000 keys    8.5    9.7       6.5    9.1   24.1   13.9
+//   B  1,  2000        12.9   10.0       9.6    9.3   43.4   14.1
+//   B  4,  4000        21.8   10.5      15.8    9.7   81.9   14.7
+//   B 16,  2000        13.6   13.0       9.8   11.1   43.4   20.3
+//   B 16,  4000        22.8   18.0      16.1   13.6   82.4   32.4
+//   B 32,  2000        14.5   20.6      10.4   14.3   43.5   34.0
 // That is for sequences of one length, which is all that the host knows.  Where one of them may be
 // far longer, its workgroup alone may walk for long, so a call of more than 1024 steps (140 us)
 // is cut whatever the batch would take together; the chunks are made of the lengths there are, about
@@ -220,21 +221,21 @@ void launch_kind(PagedAttnArgs a, hipStream_t st) {
 // key heads and blocks of one sequence are a round of workgroups by themselves (the partial results
 // are twice its queries): there is nothing to gain.
 //                                           unsplit   split
-//   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     771    57
-//   B 40, one of 131072, 39 of 1000,      1,     28/4           575    39
-//   B 200, one of 40000, 199 of 1000,     1,     32/8           294   114
-//   B 20, 33000 each,                     1,     28/4           223   132
-//   B 20, 33000 each,                     1,     32/8           251   260
-//   B 64, 33000 each,                     8,     28/4           580   595
-//   B 64, 1000 each, max_cached 131072,   1,     32/8            23    26   (what a loose bound costs)
+//   B 20, one of 131072 keys, 19 of 1000, 1 row, 32/8 heads     772    59
+//   B 40, one of 131072, 39 of 1000,      1,     28/4           578    38
+//   B 200, one of 40000, 199 of 1000,     1,     32/8           296   113
+//   B 20, 33000 each,                     1,     28/4           217   128
+//   B 20, 33000 each,                     1,     32/8           245   247
+//   B 64, 33000 each,                     8,     28/4           575   588
+//   B 64, 1000 each, max_cached 131072,   1,     32/8            24    28   (what a loose bound costs)
 AttnSplit attn8_split(int fp32, int batch, int G, int hq, int hkv, int hd, int max_cached, int fresh) {
   const Kind kind = kind_of(fp32, batch, G, hq, hkv, hd);
   if (kind == Kind::WIDE) return AttnSplit{0, 0, batch, TILE};
   const long ncol = (long)G * (hq / hkv), groups = hkv * (kind == Kind::COL1 ? (ncol + 15) / 16 : (ncol + 31) / 32);
   const long steps = ((long)max_cached + STEP - 1) / STEP + ((fresh ? G : 0) + STEP - 1) / STEP;
   AttnSplit s{0, 2 * NWAVE, batch, STEP};
-  // As many workgroups as CUs, where that is a good many chunks to a sequence (B 16, 8000 keys, 1 row, 28/4 heads: 26 us, 28
-  // with four to a CU; B 4, 70001 to 131072: 64, 68).  Else one round of what the CUs hold: cutting B sequences by one
+  // As many workgroups as CUs, where that is a good many chunks to a sequence (B 16, 8000 keys, 1 row, 28/4 heads: 27 us, 29
+  // with four to a CU; B 4, 70001 to 131072: 75.5, 80.8).  Else one round of what the CUs hold: cutting B sequences by one
   // length leaves up to B chunks more than that length divides out (the first of the table above: 71, 57).
   const long round = 256 * (fp32 ? 3 : 256 / groups >= 4L * batch ? 1 : kind == Kind::COL1 ? 4 : 2);
   long target = round / groups - batch;

@@ -20,11 +20,13 @@
 //            of the bin of the cut alone, and the weight of each piece's higher bins
 //   finish   cuts the list and draws: within the list, or in a piece, 256 tokens of it, a token
 // A sixth one does whole rows in one workgroup, where the others found that they cannot: a logit that is infinite or
-// more than 95 nats above m0, or a list too long (one value tens of thousands of times).
+// more than 95 T above m0 (at T = 0.05, 4.75: the row's maximum is often that far above its first 4096 tokens'; or these all have
+// a mask's finite value), or a list too long (one value tens of thousands of times).  256 rows of 126464, one value in 3161 6 higher,
+// top-p: T = 0.1 57 us, 0.05 144; beginning with 5000 masked tokens, T = 1 241, else 100.
 //
-// What bounds it: of many rows the two passes, instructions (about 17 a token in survey, of them 12 in 64 bits) and reads
-// alike (1024 rows of 152064 fp32 with filters of every kind: 134 us, 4.6 TB/s, and 55 us for the pieces that can hold a kept
-// token; 2048 such rows 499 us); of one row the launches and cold instructions, 28 us.  One workgroup a row, as a single
+// What bounds it: of many rows the first pass's reads (1024 rows of 152064 fp32 with filters of every kind: 136 us, 4.6 TB/s),
+// then the second pass over the pieces that can hold a kept token (59 us) and the launches beside them (59 us; 2048 such rows
+// 503 us in all); of one row the six launches and cold instructions, 30 us.  One workgroup a row, as a single
 // launch, took 3566 us and 330 us.  Calls split into groups of rows whose logits stay in the last-level cache for collect:
 // collect is no faster, and the short launches are paid for each group (797 us against 628, before pieces were passed over).
 #include <algorithm>
